@@ -18,7 +18,10 @@
  *   - on the host, the expert significance of Eq. (1) and the precision of
  *     each expert from Alg. 1 (Sec. III-B, Sec. IV-A),
  *   - dequantization fused with the matrix-core contraction (Sec. V-B
- *     "Channel-Grained Dequantization"), applied to the routed expert FFN.
+ *     "Channel-Grained Dequantization"), applied to the routed expert FFN,
+ * and what a decoding program needs around that layer: few-token products with
+ * packed 4-bit weights, the norms around a block with its gate and residual, and
+ * attention of drafted tokens over a paged cache ("Decoder block" below).
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -117,7 +120,8 @@ extern "C" {
 #define MOE_ERR_ALIGN     -3  /* a pointer that must be 16-byte aligned is not          */
 #define MOE_ERR_WORKSPACE -4  /* workspace NULL or smaller than the size helper returns */
 #define MOE_ERR_SLOT      -5  /* switch slot out of range, duplicated, or two slots
-                                 naming the same (expert, row)                          */
+                                 naming the same (expert, row); a cache page, position
+                                 or draft index out of range (device status word)       */
 #define MOE_ERR_RANGE     -6  /* a value outside fp16's range: a scale in moe_quant_pack
                                  or moe_requant_channels, an activation or hidden value
                                  of the FFN's fp16 operand path (device status words) */
@@ -499,6 +503,186 @@ int moe_allocate_bits(const double* x, const double* share, int32_t n,
                       const int32_t* levels, int32_t c, double m, double eps,
                       int32_t max_iter, double alpha, int32_t* bits, double* V,
                       double* U, int32_t* rounds);
+
+/* ------------------------------------------------------------------------
+ * Decoder block
+ * ------------------------------------------------------------------------
+ * The steps around the expert FFN in one decoder block, for decoding with
+ * drafted tokens: project (moe_quant_linear), rotate and store
+ * (moe_cache_append), attend (moe_tree_attention), project, add and normalize
+ * (moe_block_norm), route and run the experts (above), add and normalize; and,
+ * once the drafts have been checked, keep the accepted ones (moe_cache_keep).
+ * The conventions above hold: caller's buffers, `stream`, host validation.
+ * Tensors may differ in type; MOE_TYPE_* names the type of each.
+ */
+#define MOE_TYPE_BF16 0
+#define MOE_TYPE_FP16 1
+#define MOE_TYPE_FP32 2
+
+/*
+ * moe_quant_linear -- few-token product with packed 4-bit weights:
+ *   y[t][r] = bias[r] + sum_c s(r, j) * (q(r, c) - z(r, j)) * x[t][c],  j = c / group,
+ * the projections around the expert FFN, over the rows moe_quant_pack writes.
+ *
+ *   x         device bf16 or fp16 [T][ld_x], x_type its type; 16-byte aligned rows
+ *             (x and ld_x*2).  K values of each row are used.
+ *   codes     device [R][ld_codes] packed 4-bit rows; 16-byte aligned rows.
+ *             moe_code_row_words(K, 4) is a stride that spreads rows over channels.
+ *   sz        device; the {s16, z} word of (row r, group j) is
+ *             sz[r*sz_row_stride + j*sz_group_stride].
+ *   bits      4 (MOE_ERR_BITS otherwise).   group  64 or 128; K % group == 0.
+ *   bias      device fp32 [R] or NULL.
+ *   y         device [T][ld_y] of y_type: x_type or MOE_TYPE_FP32.
+ * Sums are fp32 over exact products: the integer codes are exact operands, and
+ * each group's scale and zero point are applied to its fp32 partial sum.  The
+ * order of the sums depends on T, R and K only, so results are bitwise
+ * reproducible.  An infinite or NaN activation makes its token's outputs NaN or
+ * infinite and no other token's.  Meant for decoding (up to a few hundred
+ * tokens); any T gives right results, the weights being read once per 64 tokens.
+ */
+int moe_quant_linear(const void* x, int32_t x_type, int64_t ld_x, int32_t T, int32_t K,
+                     const uint32_t* codes, int64_t ld_codes,
+                     const uint32_t* sz, int64_t sz_row_stride, int64_t sz_group_stride,
+                     int32_t R, int32_t bits, int32_t group, const float* bias,
+                     void* y, int32_t y_type, int64_t ld_y, void* stream);
+
+/*
+ * moe_block_norm -- what stands between two blocks of a decoder layer, in one
+ * pass: the norm after a block, its gate, the scaled residual add, and the norm
+ * before the next block.  For each token t and channel c < d:
+ *   a = y * rsqrt(mean_c(y^2) + eps) * w_post   (a = y when w_post is NULL)
+ *   v = residual_scale * r + branch_scale * gate * a
+ *       (gate = 1 when NULL; v = residual_scale * r when y is NULL)
+ *   r_out = v,   h = v * rsqrt(mean_c(v^2) + eps) * w_pre   (w_pre NULL: 1)
+ *
+ *   y       device [T][ld_y] of y_type or NULL: the block's output (for an expert
+ *           FFN, moe_unpermute_combine's fp32 y).
+ *   r       device [T][ld_r] of r_type: the residual stream.
+ *   gate    device, gate_type: element (t, c) at t*gate_row_stride +
+ *           c*gate_col_stride, gate_col_stride 0 or 1 (per channel: strides 0, 1;
+ *           per token: s, 0; per element: s, 1).
+ *   w_post, w_pre   device fp32 [d] or NULL.
+ *   r_out   device [T][ld_r_out] of r_type or NULL; may be r itself (same ld).
+ *   h       device [T][ld_h] of h_type or NULL; may be r or y itself where type
+ *           and ld agree.  r_out and h must not overlap each other.
+ * Types are any MOE_TYPE_*; pointers need their type's alignment only.  Norms and
+ * sums are fp32; r_out and h are rounded once (h from the unrounded v).  d up to
+ * 2^30.  eps >= 0.  Results are bitwise reproducible.
+ */
+int moe_block_norm(const void* y, int32_t y_type, int64_t ld_y,
+                   const void* r, int32_t r_type, int64_t ld_r, int32_t T, int32_t d,
+                   const float* w_post, const void* gate, int32_t gate_type,
+                   int64_t gate_row_stride, int64_t gate_col_stride,
+                   float branch_scale, float residual_scale, const float* w_pre, float eps,
+                   void* r_out, int64_t ld_r_out, void* h, int32_t h_type, int64_t ld_h,
+                   void* stream);
+
+/*
+ * One layer's paged key/value cache.
+ *
+ * Slot o of page p holds, for key/value head g, the key at
+ * k[((p*n_heads + g)*page_size + o)*head_dim + c] and the value, transposed
+ * inside the page, at v[((p*n_heads + g)*head_dim + c)*page_size + o]: 8 slots of
+ * one value channel are 16 bytes, as the matrix cores take them.  Token i of a
+ * sequence lives in page table[i / page_size], slot i % page_size.  Slots that no
+ * token has been written to may hold anything, NaN included.
+ */
+typedef struct moe_cache {
+  void*   k;            /* device, 16-byte aligned */
+  void*   v;            /* device, 16-byte aligned */
+  int32_t n_pages;
+  int32_t n_heads;      /* key/value heads */
+  int32_t head_dim;     /* 64, 128 or 256 */
+  int32_t page_size;    /* a power of two, 32 to 1024 */
+  int32_t type;         /* MOE_TYPE_BF16 or MOE_TYPE_FP16 */
+  int32_t reserved0;
+} moe_cache_t;
+
+/*
+ * The batch that the three cache calls share: n_seqs sequences; sequence b has
+ * cache_len[b] tokens in the cache (device int32 [n_seqs]), its new (drafted)
+ * tokens are rows new_off[b] .. new_off[b+1] - 1 of the call's token-major
+ * arrays (device int32 [n_seqs + 1], ascending, at most n_tokens), and its pages
+ * are table[b*max_pages ...] (device int32 [n_seqs][max_pages], each in [0,
+ * n_pages)).  New token i of the sequence lives in slot cache_len[b] + i.
+ * max_new is the most new tokens of any sequence, known on the host.  A
+ * length, page, position or draft index outside its range is never followed:
+ * what it names is skipped, and `status` (device int32 or NULL, never cleared by
+ * the library) is set to MOE_ERR_SLOT.
+ */
+
+/*
+ * moe_cache_append -- rotate the new tokens' queries and keys by their
+ * positions and store keys and values in the cache.
+ *   q, k, v    device [n_tokens][ld] of the cache's type, heads side by side
+ *              (n_q_heads*head_dim, n_heads*head_dim values of a row): the three
+ *              may be parts of one projection's output rows.  q may be NULL.
+ *   positions  device int32 [n_tokens] or NULL (cache_len[b] + i).
+ *   cos, sin   device fp32 [max_pos][rot_dim/2], or both NULL: no rotation.
+ *              The first rot_dim (even, <= head_dim) values of each head turn in
+ *              pairs (c, c + rot_dim/2), or (2c, 2c + 1) when interleaved != 0:
+ *              (a, b) -> (a cos - b sin, a sin + b cos), fp32, rounded once.
+ *   q_out      device [n_tokens][ld_q_out], NULL when q is; may be q itself (same ld).
+ */
+int moe_cache_append(const moe_cache_t* C, const int32_t* table, int32_t max_pages,
+                     const int32_t* cache_len, int32_t n_seqs, const int32_t* new_off,
+                     int32_t n_tokens, int32_t max_new,
+                     const void* q, int64_t ld_q, int32_t n_q_heads,
+                     const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                     const int32_t* positions, const float* cos, const float* sin,
+                     int32_t rot_dim, int32_t max_pos, int32_t interleaved,
+                     void* q_out, int64_t ld_q_out, int32_t* status, void* stream);
+
+/*
+ * moe_tree_attention_plan -- the number of parts the keys are split into and the
+ * workspace bytes of moe_tree_attention for this batch (0 when it is 1).  Depends only on
+ * host-known sizes; max_len is the most cached plus new tokens of any sequence
+ * as far as the host knows it (a wrong value costs time, never correctness, as
+ * long as plan and call are given the same one).
+ */
+int moe_tree_attention_plan(const moe_cache_t* C, int32_t n_q_heads, int32_t n_seqs,
+                            int32_t max_new, int32_t max_len, int32_t* n_split, size_t* ws_bytes);
+
+/*
+ * moe_tree_attention -- attention of each sequence's new tokens over its cached
+ * tokens and over those new tokens that its mask names, all read from the cache
+ * (moe_cache_append first):
+ *   out[t][h] = sum_j softmax_j(scale * q[t][h] . k_j) v_j
+ * over the slots j that token t sees: every j < cache_len[b], and cache_len[b] + m
+ * where bit m % 64 of mask[t*mask_words + m / 64] is set (device uint64
+ * [n_tokens][mask_words]; for a tree of drafts, the token itself and its
+ * ancestors).  mask NULL: a chain, m <= the token's own index.  Query head h reads
+ * key/value head h / (n_q_heads / n_heads).  A token that sees nothing gets zeros.
+ * What a token does not see has no effect on it, NaN and infinities included.
+ *   q, out    device [n_tokens][ld] of the cache's type, heads side by side;
+ *             rows of q 16-byte aligned.  out must not overlap q or the cache.
+ *   ws        device workspace of moe_tree_attention_plan's bytes for the same
+ *             sizes (NULL when that is 0); scratch between calls.
+ * Scores, softmax and sums are fp32; the softmax weights enter the second
+ * product rounded to the cache's type, as its matrix operand.  n_q_heads is a multiple of
+ * n_heads, at most 64 times it.  Results are bitwise reproducible.
+ */
+int moe_tree_attention(const moe_cache_t* C, const int32_t* table, int32_t max_pages,
+                       const int32_t* cache_len, int32_t n_seqs, const int32_t* new_off,
+                       int32_t n_tokens, int32_t max_new, int32_t max_len,
+                       const void* q, int64_t ld_q, int32_t n_q_heads,
+                       const uint64_t* mask, int32_t mask_words, float scale,
+                       void* out, int64_t ld_out, int32_t* status,
+                       void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * moe_cache_keep -- keep the accepted drafts: for each sequence b the rows of new
+ * tokens keep[b*max_keep + j], j < n_keep[b] (device int32; indices into the
+ * sequence's new tokens, strictly ascending, as a tree's path is), move to slots
+ * cache_len[b] + j.  A list that is not ascending or names a token the sequence
+ * does not have moves nothing (MOE_ERR_SLOT in status).
+ *   len_out   device int32 [n_seqs] or NULL: cache_len[b] + n_keep[b] (cache_len[b]
+ *             where nothing moves for a bad list); must not be cache_len itself.
+ */
+int moe_cache_keep(const moe_cache_t* C, const int32_t* table, int32_t max_pages,
+                   const int32_t* cache_len, int32_t n_seqs, const int32_t* new_off,
+                   const int32_t* keep, int32_t max_keep, const int32_t* n_keep,
+                   int32_t* len_out, int32_t* status, void* stream);
 
 /* Human-readable name of a status code. */
 const char* moe_status_str(int status);

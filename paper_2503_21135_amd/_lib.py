@@ -17,6 +17,7 @@ KIND_GATE, KIND_UP, KIND_DOWN = 0, 1, 2
 MAX_EXPERTS = 256
 MAX_TOPK = 16
 NOALLOC_SCRATCH_BYTES = 64 << 20
+TYPE_BF16, TYPE_FP16, TYPE_FP32 = 0, 1, 2
 
 EXPORTS = (
     "moe_quant_pack", "moe_code_row_words", "moe_route_permute", "moe_route_workspace_bytes",
@@ -25,6 +26,8 @@ EXPORTS = (
     "moe_set_channel_switch",
     "moe_requant_channels", "moe_unpermute_combine", "moe_status_str",
     "moe_expert_significance", "moe_allocate_bits",
+    "moe_quant_linear", "moe_block_norm",
+    "moe_cache_append", "moe_cache_keep", "moe_tree_attention", "moe_tree_attention_plan",
 )
 
 
@@ -48,6 +51,13 @@ class LayerDesc(C.Structure):
     ]
 
 
+class CacheDesc(C.Structure):
+    _fields_ = [
+        ("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int32), ("n_heads", C.c_int32),
+        ("head_dim", C.c_int32), ("page_size", C.c_int32), ("type", C.c_int32), ("reserved0", C.c_int32),
+    ]
+
+
 class MoEError(RuntimeError):
     pass
 
@@ -64,7 +74,8 @@ def load() -> C.CDLL:
         raise MoEError("libmoe_quant.so is not built (run __graft_entry__.build() or "
                        "python paper_2503_21135_amd/build.py); there is no CPU fallback")
     L = C.CDLL(LIB_PATH)
-    vp, i32, i64, sz_t = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
+    vp, i32, i64, sz_t, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t, C.c_float
+    cache, batch = C.POINTER(CacheDesc), [vp, i32, vp, i32, vp]   # table, max_pages, cache_len, n_seqs, new_off
     sig = {
         "moe_quant_pack": (C.c_int, [vp, i64, i32, i32, i32, i32, vp, i32, vp, i64, vp, i64, i64, vp, vp]),
         "moe_route_permute": (C.c_int, [vp, i32, i32, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp,
@@ -85,6 +96,16 @@ def load() -> C.CDLL:
         "moe_expert_significance": (C.c_int, [vp, vp, i32, i32, i32, vp, vp]),
         "moe_allocate_bits": (C.c_int, [vp, vp, i32, vp, i32, C.c_double, C.c_double, i32,
                                         C.c_double, vp, vp, vp, C.POINTER(i32)]),
+        "moe_quant_linear": (C.c_int, [vp, i32, i64, i32, i32, vp, i64, vp, i64, i64, i32, i32, i32, vp,
+                                       vp, i32, i64, vp]),
+        "moe_block_norm": (C.c_int, [vp, i32, i64, vp, i32, i64, i32, i32, vp, vp, i32, i64, i64, f32, f32,
+                                     vp, f32, vp, i64, vp, i32, i64, vp]),
+        "moe_cache_append": (C.c_int, [cache] + batch + [i32, i32, vp, i64, i32, vp, i64, vp, i64, vp, vp, vp,
+                                                         i32, i32, i32, vp, i64, vp, vp]),
+        "moe_tree_attention_plan": (C.c_int, [cache, i32, i32, i32, i32, C.POINTER(i32), C.POINTER(sz_t)]),
+        "moe_tree_attention": (C.c_int, [cache] + batch + [i32, i32, i32, vp, i64, i32, vp, i32, f32, vp, i64,
+                                                           vp, vp, sz_t, vp]),
+        "moe_cache_keep": (C.c_int, [cache] + batch + [vp, i32, vp, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)

@@ -14,7 +14,7 @@ from typing import Optional, Tuple
 import numpy as np
 import torch
 
-from ._lib import LayerDesc, MoEError, check, load
+from ._lib import TYPE_BF16, TYPE_FP16, TYPE_FP32, CacheDesc, LayerDesc, MoEError, check, load
 
 
 def _p(t: Optional[torch.Tensor]):
@@ -165,6 +165,199 @@ def moe_unpermute_combine(o: torch.Tensor, n_split: int, inv_perm: torch.Tensor,
     st = load().moe_unpermute_combine(_p(o), n_split, split_stride, _p(inv_perm), _p(topk_w),
                                       T, k, S, d, _p(y), _s(stream))
     check(st, "moe_unpermute_combine")
+
+
+# ---------------------------------------------------------------------------
+# decoder block around the expert FFN
+# ---------------------------------------------------------------------------
+# These calls take a few microseconds on the device, so their marshalling passes
+# plain integers (ctypes takes them for pointers) and checks only what the C entry
+# points cannot see: types, shapes and strides of the tensors.
+_TYPES = {torch.bfloat16: TYPE_BF16, torch.float16: TYPE_FP16, torch.float32: TYPE_FP32}
+
+
+def _type(t: torch.Tensor, what: str) -> int:
+    ty = _TYPES.get(t.dtype)
+    if ty is None:
+        raise MoEError("%s must be bfloat16, float16 or float32, not %s" % (what, t.dtype))
+    return ty
+
+
+def _stream(stream) -> int:
+    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+
+
+def _rows(t: torch.Tensor, shape: tuple, what: str) -> int:
+    """Data pointer of a device tensor of this shape whose rows are contiguous."""
+    if t.shape != shape:
+        raise MoEError("%s has shape %s, not %s" % (what, tuple(t.shape), tuple(shape)))
+    if not t.is_cuda:
+        raise MoEError("%s is not a device tensor" % what)
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise MoEError("%s needs contiguous rows" % what)
+    return t.data_ptr()
+
+
+def _flat(t: Optional[torch.Tensor], shape: tuple, dtype: torch.dtype, what: str):
+    """Data pointer of a contiguous device tensor (None for None)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+        raise MoEError("%s must be a contiguous %s device tensor of shape %s" % (what, dtype, tuple(shape)))
+    return t.data_ptr()
+
+
+def moe_quant_linear(x: torch.Tensor, codes: torch.Tensor, sz: torch.Tensor, y: torch.Tensor,
+                     bits: int = 4, bias: Optional[torch.Tensor] = None, stream=None) -> None:
+    """y [T][R] = x [T][K] times packed 4-bit rows (+ bias [R]).
+
+    codes  int32 [R][>= K/8], a row's words contiguous (moe_quant_pack's layout)
+    sz     int32 [K/group][R] {scale, zero} words; a transposed view of [R][K/group] works too
+    x      bfloat16 or float16; y the same type or float32
+    """
+    T, K = x.shape
+    G, R = sz.shape
+    if G < 1 or K % G:
+        raise MoEError("sz has %d groups for K = %d" % (G, K))
+    if codes.dtype != torch.int32 or sz.dtype != torch.int32 or not sz.is_cuda:
+        raise MoEError("codes and sz must be int32 device tensors")
+    if codes.dim() != 2 or codes.shape[0] != R or codes.shape[1] * 8 < K:
+        raise MoEError("codes have shape %s for %d rows of K = %d" % (tuple(codes.shape), R, K))
+    st = load().moe_quant_linear(_rows(x, (T, K), "x"), _type(x, "x"), x.stride(0) if T > 1 else K, T, K,
+                                 _rows(codes, codes.shape, "codes"), codes.stride(0) if R > 1 else codes.shape[1],
+                                 sz.data_ptr(), sz.stride(1) if R > 1 else 1, sz.stride(0) if G > 1 else R,
+                                 R, bits, K // G, _flat(bias, (R,), torch.float32, "bias"),
+                                 _rows(y, (T, R), "y"), _type(y, "y"), y.stride(0) if T > 1 else R,
+                                 _stream(stream))
+    check(st, "moe_quant_linear")
+
+
+def moe_block_norm(r: torch.Tensor, h: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
+                   w_post: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                   w_pre: Optional[torch.Tensor] = None, r_out: Optional[torch.Tensor] = None,
+                   branch_scale: float = 1.0, residual_scale: float = 1.0, eps: float = 1e-6,
+                   stream=None) -> None:
+    """Norm after a block, gate, residual add and norm before the next, for rows [T][d]:
+    v = residual_scale r + branch_scale gate rms(y) w_post;  r_out = v;  h = rms(v) w_pre.
+
+    gate is [d] (per channel), [T][1] (per token) or [T][d]; without y, v is the scaled
+    residual alone; without w_post, y is taken as it is.  r_out may be r, h may be r or y.
+    """
+    T, d = r.shape
+    one = T == 1
+    g, g_type, g_row, g_col = None, 0, 0, 0
+    if gate is not None:
+        g_type = _type(gate, "gate")
+        if gate.dim() == 1:
+            g, g_col = _rows(gate, (d,), "gate"), 1
+        elif gate.dim() == 2 and gate.shape[1] == 1 and d > 1:
+            g, g_row = _rows(gate, (T, 1), "gate"), 0 if one else gate.stride(0)
+        else:
+            g, g_row, g_col = _rows(gate, (T, d), "gate"), 0 if one else gate.stride(0), 1
+    if r_out is not None and r_out.dtype != r.dtype:
+        raise MoEError("r_out must have the type of r")
+    st = load().moe_block_norm(
+        None if y is None else _rows(y, (T, d), "y"), 0 if y is None else _type(y, "y"),
+        d if y is None or one else y.stride(0),
+        _rows(r, (T, d), "r"), _type(r, "r"), d if one else r.stride(0), T, d,
+        _flat(w_post, (d,), torch.float32, "w_post"), g, g_type, g_row, g_col, branch_scale, residual_scale,
+        _flat(w_pre, (d,), torch.float32, "w_pre"), eps,
+        None if r_out is None else _rows(r_out, (T, d), "r_out"), d if r_out is None or one else r_out.stride(0),
+        None if h is None else _rows(h, (T, d), "h"), 0 if h is None else _type(h, "h"),
+        d if h is None or one else h.stride(0), _stream(stream))
+    check(st, "moe_block_norm")
+
+
+def _heads(t: torch.Tensor, shape: tuple, dtype: torch.dtype, what: str) -> int:
+    """Data pointer of a [tokens][heads][head_dim] device tensor whose heads lie side by side."""
+    if t.shape != shape or t.dtype != dtype or not t.is_cuda:
+        raise MoEError("%s must be a %s device tensor of shape %s" % (what, dtype, tuple(shape)))
+    if t.stride(2) != 1 or (shape[1] > 1 and t.stride(1) != shape[2]):
+        raise MoEError("the heads of a token of %s must lie side by side" % what)
+    return t.data_ptr()
+
+
+def _ld(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _batch(table: torch.Tensor, lens: torch.Tensor, new_off: torch.Tensor):
+    """(table, max_pages, cache_len, n_seqs, new_off) of the three cache calls."""
+    B = lens.shape[0]
+    if table.dim() != 2:
+        raise MoEError("table must be [sequences][pages]")
+    return (_flat(table, (B, table.shape[1]), torch.int32, "table"), table.shape[1],
+            _flat(lens, (B,), torch.int32, "cache_len"), B, _flat(new_off, (B + 1,), torch.int32, "new_off"))
+
+
+_DTYPE16 = {TYPE_BF16: torch.bfloat16, TYPE_FP16: torch.float16}
+
+
+def moe_cache_append(desc: CacheDesc, table: torch.Tensor, lens: torch.Tensor, new_off: torch.Tensor,
+                     max_new: int, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
+                     q_out: Optional[torch.Tensor], positions: Optional[torch.Tensor] = None,
+                     cos: Optional[torch.Tensor] = None, sin: Optional[torch.Tensor] = None,
+                     interleaved: bool = False, status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Rotate q and k [tokens][heads][head_dim] by cos/sin [max_pos][rot_dim/2] and store
+    k and v of the new tokens in the cache."""
+    N, dt, D = k.shape[0], _DTYPE16[desc.type], desc.head_dim
+    kv = (N, desc.n_heads, D)
+    Hq = 0 if q is None else q.shape[1]
+    if (q is None) != (q_out is None) or (cos is None) != (sin is None):
+        raise MoEError("q and q_out, cos and sin come in pairs")
+    tab = (1, 0) if cos is None else tuple(cos.shape)
+    st = load().moe_cache_append(
+        C.byref(desc), *_batch(table, lens, new_off), N, max_new,
+        None if q is None else _heads(q, (N, Hq, D), dt, "q"), 0 if q is None else _ld(q), Hq,
+        _heads(k, kv, dt, "k"), _ld(k), _heads(v, kv, dt, "v"), _ld(v),
+        _flat(positions, (N,), torch.int32, "positions"), _flat(cos, tab, torch.float32, "cos"),
+        _flat(sin, tab, torch.float32, "sin"), 2 * tab[1], tab[0], int(interleaved),
+        None if q is None else _heads(q_out, (N, Hq, D), dt, "q_out"), 0 if q is None else _ld(q_out),
+        _flat(status, (1,), torch.int32, "status"), _stream(stream))
+    check(st, "moe_cache_append")
+
+
+def moe_tree_attention_plan(desc: CacheDesc, n_q_heads: int, n_seqs: int, max_new: int,
+                            max_len: int) -> Tuple[int, int]:
+    """(parts the keys are split into, workspace bytes) of moe_tree_attention."""
+    ns, wb = C.c_int32(0), C.c_size_t(0)
+    check(load().moe_tree_attention_plan(C.byref(desc), n_q_heads, n_seqs, max_new, max_len, C.byref(ns),
+                                         C.byref(wb)), "moe_tree_attention_plan")
+    return int(ns.value), int(wb.value)
+
+
+def moe_tree_attention(desc: CacheDesc, table: torch.Tensor, lens: torch.Tensor, new_off: torch.Tensor,
+                       max_new: int, max_len: int, q: torch.Tensor, out: torch.Tensor, scale: float,
+                       mask: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                       status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Attention of the new tokens q [tokens][heads][head_dim] over the cache.  mask is
+    int64 [tokens][words]: bit m of a token's words, m % 64 of word m // 64, lets it see
+    its sequence's new token m; None is a chain (each token sees itself and those before)."""
+    N, Hq, D = q.shape
+    dt = _DTYPE16[desc.type]
+    words = 0 if mask is None else mask.shape[-1]
+    if ws is not None and (not ws.is_cuda or not ws.is_contiguous()):
+        raise MoEError("ws must be a contiguous device tensor")
+    st = load().moe_tree_attention(
+        C.byref(desc), *_batch(table, lens, new_off), N, max_new, max_len,
+        _heads(q, (N, Hq, desc.head_dim), dt, "q"), _ld(q), Hq, _flat(mask, (N, words), torch.int64, "mask"),
+        words, scale, _heads(out, (N, Hq, D), dt, "out"), _ld(out), _flat(status, (1,), torch.int32, "status"),
+        None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel() * ws.element_size(),
+        _stream(stream))
+    check(st, "moe_tree_attention")
+
+
+def moe_cache_keep(desc: CacheDesc, table: torch.Tensor, lens: torch.Tensor, new_off: torch.Tensor,
+                   keep: torch.Tensor, n_keep: torch.Tensor, len_out: Optional[torch.Tensor] = None,
+                   status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Move the accepted drafts keep [sequences][max_keep] (the first n_keep of each row,
+    ascending) together behind the cached tokens."""
+    B = lens.shape[0]
+    st = load().moe_cache_keep(
+        C.byref(desc), *_batch(table, lens, new_off), _flat(keep, (B, keep.shape[-1]), torch.int32, "keep"),
+        keep.shape[-1], _flat(n_keep, (B,), torch.int32, "n_keep"), _flat(len_out, (B,), torch.int32, "len_out"),
+        _flat(status, (1,), torch.int32, "status"), _stream(stream))
+    check(st, "moe_cache_keep")
 
 
 # ---------------------------------------------------------------------------

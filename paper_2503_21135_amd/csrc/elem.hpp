@@ -1,0 +1,57 @@
+// elem.hpp -- the element types of the decoder-block operators (MOE_TYPE_*):
+// reading as fp32, and rounding to a type once (round to nearest even; NaN stays
+// NaN, and fp16 overflow becomes infinity).
+#pragma once
+
+#include "common.hpp"
+
+namespace moe {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+inline int type_bytes(int t) { return t == MOE_TYPE_FP32 ? 4 : 2; }
+inline bool valid_type(int t) { return t == MOE_TYPE_BF16 || t == MOE_TYPE_FP16 || t == MOE_TYPE_FP32; }
+inline bool valid_type16(int t) { return t == MOE_TYPE_BF16 || t == MOE_TYPE_FP16; }
+inline bool aligned_to(const void* p, int bytes) {
+  return (reinterpret_cast<uintptr_t>(p) & static_cast<uintptr_t>(bytes - 1)) == 0;
+}
+
+template <int TYPE> struct ElemOf;
+template <> struct ElemOf<MOE_TYPE_BF16> { typedef __bf16 type; };
+template <> struct ElemOf<MOE_TYPE_FP16> { typedef _Float16 type; };
+template <> struct ElemOf<MOE_TYPE_FP32> { typedef float type; };
+template <int TYPE> using elem_t = typename ElemOf<TYPE>::type;
+
+// two values as one word of a 16-bit type
+template <int TYPE>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  if constexpr (TYPE == MOE_TYPE_BF16) return __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(a), static_cast<__bf16>(b)});
+  else return __builtin_bit_cast(uint32_t, f16x2{static_cast<_Float16>(a), static_cast<_Float16>(b)});
+}
+
+template <int TYPE>
+__device__ __forceinline__ float half_lo(uint32_t w) {
+  if constexpr (TYPE == MOE_TYPE_BF16) return bf16_lo(w);
+  else return fp16_bits_to_f32(w & 0xFFFFu);
+}
+template <int TYPE>
+__device__ __forceinline__ float half_hi(uint32_t w) {
+  if constexpr (TYPE == MOE_TYPE_BF16) return bf16_hi(w);
+  else return fp16_bits_to_f32(w >> 16);
+}
+
+// the same with the type known at run time only
+__device__ __forceinline__ float load_elem(const void* p, int64_t i, int type) {
+  if (type == MOE_TYPE_FP32) return static_cast<const float*>(p)[i];
+  if (type == MOE_TYPE_BF16) return static_cast<float>(static_cast<const __bf16*>(p)[i]);
+  return static_cast<float>(static_cast<const _Float16*>(p)[i]);
+}
+__device__ __forceinline__ void store_elem(void* p, int64_t i, int type, float v) {
+  if (type == MOE_TYPE_FP32) static_cast<float*>(p)[i] = v;
+  else if (type == MOE_TYPE_BF16) static_cast<__bf16*>(p)[i] = static_cast<__bf16>(v);
+  else static_cast<_Float16*>(p)[i] = static_cast<_Float16>(v);
+}
+
+}  // namespace moe

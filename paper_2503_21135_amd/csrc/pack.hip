@@ -445,7 +445,7 @@ extern "C" const char* moe_status_str(int status) {
     case MOE_ERR_BITS: return "bit-width not in {2,3,4,6,8} (or 16 where allowed)";
     case MOE_ERR_ALIGN: return "pointer or stride not 16-byte aligned";
     case MOE_ERR_WORKSPACE: return "workspace missing or too small";
-    case MOE_ERR_SLOT: return "bad switch slot list";
+    case MOE_ERR_SLOT: return "bad switch slot list, or a cache page, position or draft index out of range";
     case MOE_ERR_RANGE: return "fp16 scale overflow";
     case MOE_ERR_HIP: return "HIP error";
     default: return "unknown status";
