@@ -116,6 +116,18 @@ def test_linear_bad_token_stays_alone(T, bad):
     assert torch.equal(y[keep], y2[keep])
 
 
+@pytest.mark.parametrize("T", [1, 2, 3, 20])
+@pytest.mark.parametrize("size", [1e-6, 1e-3, 300.0])
+def test_linear_small_and_large_activations(T, size):
+    """fp16 activations in and below the normal range, and large ones."""
+    codes, sz, w, mag = packed(200, 1024, 128, 13)
+    x = (size * torch.randn(T, 1024, device="cuda", generator=gen(T))).to(FP16)
+    y = torch.empty(T, 200, device="cuda")
+    P().moe_quant_linear(x, codes, sz, y)
+    want = x.double() @ w.t()
+    within(y, want, linear_bound(x, mag, 1024, FP32, want), "size %g" % size)
+
+
 def test_linear_rows_past_32_bits():
     K, group, ld = 256, 64, 1 << 30
     codes, sz, w, mag = packed(4, K, group, 12)
