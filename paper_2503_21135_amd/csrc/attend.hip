@@ -182,8 +182,7 @@ __global__ void __launch_bounds__(kWaves * kWave, D * RT <= 256 ? 2 : 1) attend_
         for (int e = 0; e < 8; e++) x[e] = see[rt] >> e & 1 ? x[e] : -INFINITY;
       }
       float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-      mx = fmaxf(mx, __shfl_xor(mx, 16));
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      mx = rows_max(mx);
       const float m2 = fmaxf(m[rt], mx), ms = m2 == -INFINITY ? 0.f : m2;
       if (__any(m2 > m[rt])) {
         const float f = __builtin_amdgcn_exp2f(m[rt] - ms);
@@ -275,8 +274,7 @@ __global__ void __launch_bounds__(kWaves * kWave, D * RT <= 256 ? 2 : 1) attend_
   // join the waves that shared the rows: common maximum, then the sums in wave order
 #pragma unroll
   for (int rt = 0; rt < RT; rt++) {
-    l[rt] += __shfl_xor(l[rt], 16);
-    l[rt] += __shfl_xor(l[rt], 32);
+    l[rt] = rows_sum(l[rt]);
     if (grp == 0) {
       stats[wave][rt][col][0] = m[rt];
       stats[wave][rt][col][1] = l[rt];

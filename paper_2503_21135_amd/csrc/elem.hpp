@@ -54,4 +54,47 @@ __device__ __forceinline__ void store_elem(void* p, int64_t i, int type, float v
   else static_cast<_Float16*>(p)[i] = static_cast<_Float16>(v);
 }
 
+// Reductions across lanes in vector registers alone (no pass through LDS).  A row is 16
+// lanes; the swaps exchange odd rows of one register with even rows of the other, and
+// its halves, so that of a register and its copy they leave each lane's own and its
+// partner's value.
+__device__ __forceinline__ float other_row(float v, float& own) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  own = __uint_as_float(r[0]);
+  return __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float other_half(float v, float& own) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  own = __uint_as_float(r[0]);
+  return __uint_as_float(r[1]);
+}
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xF, 0xF, true));
+}
+
+// over the four lanes of equal lane % 16, on all of them
+__device__ __forceinline__ float rows_sum(float v) {
+  float a;
+  float b = other_row(v, a);
+  v = a + b;
+  b = other_half(v, a);
+  return a + b;
+}
+__device__ __forceinline__ float rows_max(float v) {
+  float a;
+  float b = other_row(v, a);
+  v = fmaxf(a, b);
+  b = other_half(v, a);
+  return fmaxf(a, b);
+}
+// over the wave, on every lane: quads, quads of 8, halves of a row, rows
+__device__ __forceinline__ float wave_sum(float v) {
+  v += dpp<0xB1>(v);    // lane ^ 1
+  v += dpp<0x4E>(v);    // lane ^ 2
+  v += dpp<0x141>(v);   // mirrored within 8
+  v += dpp<0x140>(v);   // mirrored within 16
+  return rows_sum(v);
+}
+
 }  // namespace moe

@@ -115,8 +115,7 @@ __global__ void __launch_bounds__(kVecWaves * kWave) linear_vec_kernel(LinearArg
   for (int r = 0; r < RW; r++)
 #pragma unroll
     for (int t = 0; t < T; t++) {
-      float v = acc[r][t];
-      for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+      const float v = wave_sum(acc[r][t]);
       if (lane == 0 && r0 + r < a.R) store_y(a, t, r0 + r, v);
     }
 }
