@@ -616,10 +616,11 @@ typedef struct moe_cache {
  * positions and store keys and values in the cache.
  *   q, k, v    device [n_tokens][ld] of the cache's type, heads side by side
  *              (n_q_heads*head_dim, n_heads*head_dim values of a row): the three
- *              may be parts of one projection's output rows.  q may be NULL.
+ *              may be parts of one projection's output rows.  q may be NULL;
+ *              n_q_heads is a multiple of n_heads.
  *   positions  device int32 [n_tokens] or NULL (cache_len[b] + i).
  *   cos, sin   device fp32 [max_pos][rot_dim/2], or both NULL: no rotation.
- *              The first rot_dim (even, <= head_dim) values of each head turn in
+ *              The first rot_dim (a multiple of 16, <= head_dim) values of each head turn in
  *              pairs (c, c + rot_dim/2), or (2c, 2c + 1) when interleaved != 0:
  *              (a, b) -> (a cos - b sin, a sin + b cos), fp32, rounded once.
  *   q_out      device [n_tokens][ld_q_out], NULL when q is; may be q itself (same ld).
