@@ -69,7 +69,10 @@ def linear_bound(x, mag, K, out_type, want):
     (17, 1000, 320, 64, FP16, FP32, True), (31, 33, 4096, 128, BF16, FP32, True), (33, 97, 896, 128, FP16, FP32, False),
     (48, 640, 2048, 128, BF16, BF16, True), (64, 2049, 512, 64, BF16, FP32, False), (65, 31, 128, 64, FP16, FP32, True),
     (130, 300, 1408, 128, BF16, FP32, True), (1000, 70, 256, 64, FP16, FP16, False), (1, 32000, 256, 128, BF16, FP32, False),
-    (4, 64, 14336, 128, BF16, FP32, False), (2, 40, 14336, 64, FP16, FP32, False), (1, 130, 11008, 64, BF16, FP32, True)])
+    (4, 64, 14336, 128, BF16, FP32, False), (2, 40, 14336, 64, FP16, FP32, False), (1, 130, 11008, 64, BF16, FP32, True),
+    (2, 8200, 192, 64, BF16, BF16, False), (9, 8193, 320, 64, FP16, FP32, False), (30, 8209, 256, 128, BF16, FP32, True),
+    (40, 9001, 448, 64, BF16, FP32, False), (64, 20500, 384, 128, FP16, FP32, True), (36, 20481, 192, 64, BF16, BF16, False),
+    (6, 5000, 3200, 64, FP16, FP32, False), (70, 20490, 128, 128, BF16, FP32, False)])
 def test_linear(T, R, K, group, xt, yt, bias):
     codes, sz, w, mag = packed(R, K, group, T * 7 + R)
     x = torch.randn(T, K, device="cuda", generator=gen(5))
