@@ -183,19 +183,17 @@ def _type(t: torch.Tensor, what: str) -> int:
     return ty
 
 
-def _stream(stream) -> int:
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+def _stream(stream, t: torch.Tensor) -> int:
+    """Handle of the stream to work on: the current one of t's device unless given (asked
+    for as a number: the Stream object of torch.cuda.current_stream costs 3 us)."""
+    return torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else stream.cuda_stream
 
 
 def _rows(t: torch.Tensor, shape: tuple, what: str) -> int:
     """Data pointer of a device tensor of this shape whose rows are contiguous."""
-    if t.shape != shape:
-        raise MoEError("%s has shape %s, not %s" % (what, tuple(t.shape), tuple(shape)))
-    if not t.is_cuda:
-        raise MoEError("%s is not a device tensor" % what)
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
-        raise MoEError("%s needs contiguous rows" % what)
-    return t.data_ptr()
+    if t.shape == shape and t.is_cuda and (t.is_contiguous() or t.stride(-1) == 1 or shape[-1] <= 1):
+        return t.data_ptr()
+    raise MoEError("%s must be a device tensor of shape %s with contiguous rows" % (what, tuple(shape)))
 
 
 def _flat(t: Optional[torch.Tensor], shape: tuple, dtype: torch.dtype, what: str):
@@ -228,7 +226,7 @@ def moe_quant_linear(x: torch.Tensor, codes: torch.Tensor, sz: torch.Tensor, y: 
                                  sz.data_ptr(), sz.stride(1) if R > 1 else 1, sz.stride(0) if G > 1 else R,
                                  R, bits, K // G, _flat(bias, (R,), torch.float32, "bias"),
                                  _rows(y, (T, R), "y"), _type(y, "y"), y.stride(0) if T > 1 else R,
-                                 _stream(stream))
+                                 _stream(stream, x))
     check(st, "moe_quant_linear")
 
 
@@ -264,7 +262,7 @@ def moe_block_norm(r: torch.Tensor, h: Optional[torch.Tensor] = None, y: Optiona
         _flat(w_pre, (d,), torch.float32, "w_pre"), eps,
         None if r_out is None else _rows(r_out, (T, d), "r_out"), d if r_out is None or one else r_out.stride(0),
         None if h is None else _rows(h, (T, d), "h"), 0 if h is None else _type(h, "h"),
-        d if h is None or one else h.stride(0), _stream(stream))
+        d if h is None or one else h.stride(0), _stream(stream, r))
     check(st, "moe_block_norm")
 
 
@@ -313,7 +311,7 @@ def moe_cache_append(desc: CacheDesc, table: torch.Tensor, lens: torch.Tensor, n
         _flat(positions, (N,), torch.int32, "positions"), _flat(cos, tab, torch.float32, "cos"),
         _flat(sin, tab, torch.float32, "sin"), 2 * tab[1], tab[0], int(interleaved),
         None if q is None else _heads(q_out, (N, Hq, D), dt, "q_out"), 0 if q is None else _ld(q_out),
-        _flat(status, (1,), torch.int32, "status"), _stream(stream))
+        _flat(status, (1,), torch.int32, "status"), _stream(stream, k))
     check(st, "moe_cache_append")
 
 
@@ -343,7 +341,7 @@ def moe_tree_attention(desc: CacheDesc, table: torch.Tensor, lens: torch.Tensor,
         _heads(q, (N, Hq, desc.head_dim), dt, "q"), _ld(q), Hq, _flat(mask, (N, words), torch.int64, "mask"),
         words, scale, _heads(out, (N, Hq, D), dt, "out"), _ld(out), _flat(status, (1,), torch.int32, "status"),
         None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel() * ws.element_size(),
-        _stream(stream))
+        _stream(stream, q))
     check(st, "moe_tree_attention")
 
 
@@ -356,7 +354,7 @@ def moe_cache_keep(desc: CacheDesc, table: torch.Tensor, lens: torch.Tensor, new
     st = load().moe_cache_keep(
         C.byref(desc), *_batch(table, lens, new_off), _flat(keep, (B, keep.shape[-1]), torch.int32, "keep"),
         keep.shape[-1], _flat(n_keep, (B,), torch.int32, "n_keep"), _flat(len_out, (B,), torch.int32, "len_out"),
-        _flat(status, (1,), torch.int32, "status"), _stream(stream))
+        _flat(status, (1,), torch.int32, "status"), _stream(stream, lens))
     check(st, "moe_cache_keep")
 
 

@@ -142,10 +142,10 @@ class PagedCache:
             need = self._need[key] = api.moe_tree_attention_plan(self.desc, *key)[1]
         if need == 0:
             return None
-        s = torch.cuda.current_stream() if stream is None else stream
-        ws = self._ws.get(s.cuda_stream)
+        handle = api._stream(stream, self.k)
+        ws = self._ws.get(handle)
         if ws is None or ws.numel() < need:
-            ws = self._ws[s.cuda_stream] = _empty((need,), self._bytes, s)
+            ws = self._ws[handle] = _empty((need,), self._bytes, stream)
         return ws
 
     def attend(self, q: torch.Tensor, new_off: torch.Tensor, max_new: int, max_len: int,
