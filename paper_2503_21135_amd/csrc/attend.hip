@@ -18,8 +18,8 @@ namespace moe {
 namespace cache {
 namespace {
 
-constexpr int kTile = 32;        // keys of a wave's step; divides every page size
-constexpr int kWaves = 4;
+constexpr int kTile = 32;        // keys of a step; divides every page size
+constexpr float kSlack = 8.f;    // weights stay below 2^8: finite in fp16, and exact enough in both types
 constexpr int kMaxSplit = 64;    // the joining wave holds one part's statistics per lane
 
 struct AttendArgs {
@@ -29,12 +29,17 @@ struct AttendArgs {
   float *part, *stat;   // [n_split][rows][D] sums and [n_split][rows][2] (maximum, sum) of the parts
   const uint64_t* mask;
   int64_t ld_q, ld_out;
-  float scale2;         // scale * log2(e): scores are powers of two
-  int n_q_heads, group, mask_words, n_split, row_blocks, rows_wave, units;
+  float scale2;         // |scale| * log2(e): scores are powers of two
+  uint32_t flip;        // 0x80008000 for a negative scale, which turns the queries' signs
+  int n_q_heads, group, mask_words, n_split, part_tiles, row_blocks, units;
 };
 
-// Parts of a sequence's keys, in tiles.
-__device__ __forceinline__ int tiles_per_part(int tiles, int n_split) { return (tiles + n_split - 1) / n_split; }
+// Tiles of one part of a sequence's keys: equal parts, as many as it takes for none to be
+// longer than the longest sequence's (as the host knows it), n_split at most.
+__device__ __forceinline__ int tiles_per_part(const AttendArgs& a, int tiles) {
+  const int parts = min(a.n_split, (tiles + a.part_tiles - 1) / a.part_tiles);
+  return (tiles + parts - 1) / max(parts, 1);
+}
 
 template <int TYPE>
 __device__ __forceinline__ f32x4 product(const u32x4& a, const u32x4& b, const f32x4& c) {
@@ -70,12 +75,39 @@ __device__ __forceinline__ uint32_t seen8(const AttendArgs& a, int64_t t, int i,
   return bits & 0xFFu;
 }
 
-template <int TYPE, int D, int RT>
-__global__ void __launch_bounds__(kWaves * kWave, D * RT <= 256 ? 2 : 1) attend_kernel(AttendArgs a) {
+// RW = 1: four waves on the same 16 RT rows, each with keys of its own, operands straight
+// from memory.  RW > 1: eight waves, RW of them on other rows; those read tiles of keys
+// once, side by side, into LDS, and take their operands from there (double-buffered, one
+// barrier a stage).  Straight from memory an operand has 16 rows side by side, whose
+// 16-byte pieces the vector memory path serves one per cycle: enough for one wave per tile
+// to keep up with HBM, not for several on the same one (64 drafts by 4 heads per key head
+// over 4 x 32768 slots: 310 us that way, 174 this way).
+//
+// Few rows are bound by HBM: 64 sequences of one token over up to 4096, 778 MB, 157 us and
+// 4.5 to join, 4.8 TB/s.  At 256 rows per key head (4 x 64 drafts over 32768, 88 GFLOP,
+// 418 MB: 180 us and 9 to join) a tile's matrix instructions (1024 cycles of each SIMD), vector
+// instructions (1100) and LDS reads (1150) follow each other rather than overlap, and
+// shorter sequences end before the longest.  Giving one wave of a SIMD the higher priority,
+// or the waves in their matrix instructions, left that as it was, and so did reading the
+// value operands before the softmax and four tiles a stage.
+template <int TYPE, int D, int RT, int RW>
+__global__ void __launch_bounds__(RW == 1 ? 256 : 512, D <= 128 || RW > 1 ? 2 : 1) attend_kernel(AttendArgs a) {
   typedef elem_t<TYPE> E;
-  constexpr int NC = D / 32, NV = D / 16;
-  __shared__ float stats[kWaves][RT][16][2];
-  __shared__ float sums[kWaves][16][D + 4];
+  constexpr int NC = D / 32, NV = D / 16, W = RW == 1 ? 4 : 8, KW = W / RW;
+  // tiles that a key group stages at once (with one, 204 us where two take 190, four 196),
+  // threads of a key group, and their 16-byte pieces of a stage's keys
+  constexpr int KT = RW == 1 ? 1 : std::min(2, RW * 64 / D), TG = RW * kWave, NP = KT * 4 * D / TG;
+  struct Tile {
+    u32x4 k[kTile][D / 8];    // row 16 kt + col is the operand row of lane col in tile kt; pieces and rows are
+    u32x4 v[D][kTile / 8];    // mixed so that 16 lanes' reads fall on all banks
+  };
+  struct Sums { float x[W][16][D + 4]; };
+  union Lds {
+    Tile tile[2][KW][KT];
+    Sums sums;
+  };
+  __shared__ __attribute__((aligned(16))) char lds_bytes[RW == 1 ? sizeof(Sums) : sizeof(Lds)];
+  __shared__ float stats[W][RT][16][2];
   // row blocks of a unit (sequence, head, part) sit 8 workgroups apart, on one XCD, and
   // share its keys in that XCD's L2
   const int unit = static_cast<int>(blockIdx.x) / (8 * a.row_blocks) * 8 + static_cast<int>(blockIdx.x) % 8;
@@ -84,192 +116,269 @@ __global__ void __launch_bounds__(kWaves * kWave, D * RT <= 256 ? 2 : 1) attend_
   const int part = unit % a.n_split, h = unit / a.n_split % a.b.n_heads, s = unit / a.n_split / a.b.n_heads;
   const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wr = wave % a.rows_wave, wk = wave / a.rows_wave, key_waves = kWaves / a.rows_wave;
+  const int wr = wave % RW, wk = wave / RW;
   bool ok;
   const Seq q = sequence(a.b, s, ok);
   if (!ok && threadIdx.x == 0) report(a.b, MOE_ERR_SLOT);
-  const int rows = q.n * a.group, row0 = rb * a.rows_wave * RT * 16;
+  const int rows = q.n * a.group, row0 = rb * RW * RT * 16;
   if (row0 >= rows) return;
-  const int total = q.len + q.n, tiles = (total + kTile - 1) / kTile, per = tiles_per_part(tiles, a.n_split);
-  const int t_end = min(tiles, (part + 1) * per), t_begin = part * per + wk;
-  if (part * per >= tiles) return;
+  const int total = q.len + q.n, tiles = (total + kTile - 1) / kTile, per = tiles_per_part(a, tiles);
+  if (static_cast<int64_t>(part) * per >= tiles) return;
+  const int t_first = part * per, t_end = per >= tiles - t_first ? tiles : t_first + per;
 
   u32x4 qf[RT][NC];
   int tok[RT];      // this lane's row of each row tile: its draft
 #pragma unroll
   for (int rt = 0; rt < RT; rt++) {
-    const int r = min(row0 + (wr * RT + rt) * 16 + col, rows - 1);
+    const int r = min(row0 + (wr * RT + rt) * 16 + col, rows - 1);   // a row past the last is its copy, not stored
     tok[rt] = r / a.group;
     const E* p = static_cast<const E*>(a.q) + (q.off + tok[rt]) * a.ld_q + (h * a.group + r % a.group) * D + 8 * grp;
 #pragma unroll
-    for (int c = 0; c < NC; c++) qf[rt][c] = *reinterpret_cast<const u32x4*>(p + 32 * c);
+    for (int c = 0; c < NC; c++) qf[rt][c] = *reinterpret_cast<const u32x4*>(p + 32 * c) ^ u32x4{a.flip, a.flip, a.flip, a.flip};
   }
   f32x4 o[RT][NV];
-  float m[RT], l[RT];
+  float m[RT], ms[RT], l[RT];   // maximum, the same scaled, sum
 #pragma unroll
   for (int rt = 0; rt < RT; rt++) {
-    m[rt] = -INFINITY;
+    m[rt] = ms[rt] = -INFINITY;
     l[rt] = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; v++) o[rt][v] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
   const int P = 1 << a.b.page_shift;
-  // pages of this wave's next 64 tiles, one per lane
+  // this wave's n-th tile, and the pages of 64 of them from the n-th on, one per lane
+  auto tile_of = [&](int n) { return t_first + (n / KT * KW + wk) * KT + n % KT; };
   int pages = -1;
-  auto look_up = [&](int t) {
-    const int tl = t + lane * key_waves;
+  auto look_up = [&](int n) {
+    const int tl = tile_of(n + lane);
     pages = tl < t_end ? page_of(a.b, s, tl * kTile) : 0;
     if (pages < 0) report(a.b, MOE_ERR_SLOT);
   };
   auto head_at = [&](int page) { return (static_cast<int64_t>(max(page, 0)) * a.b.n_heads + h) * P * D; };
   const int krow = 8 * (col >> 2) + (col & 3);
+  // a uniform base and a 32-bit offset per lane
+  const uint32_t k_off = krow * D + 8 * grp, v_off = col * P + 8 * grp, o_off = 4 * grp * P;
   auto load_k = [&](u32x4 (&kf)[2][NC], int page, int t) {
-    const E* p = static_cast<const E*>(a.kc) + head_at(page);
-    const int off = ((t * kTile & (P - 1)) + krow) * D + 8 * grp;
+    const E* p = static_cast<const E*>(a.kc) + head_at(page) + (t * kTile & (P - 1)) * D;
 #pragma unroll
     for (int kt = 0; kt < 2; kt++)
 #pragma unroll
-      for (int c = 0; c < NC; c++) kf[kt][c] = *reinterpret_cast<const u32x4*>(p + off + 4 * kt * D + 32 * c);
+      for (int c = 0; c < NC; c++) kf[kt][c] = *reinterpret_cast<const u32x4*>(p + (k_off + 4 * kt * D + 32 * c));
   };
   auto load_v = [&](u32x4 (&vf)[NV], int page, int t) {
-    const E* p = static_cast<const E*>(a.vc) + head_at(page);
-    const int off = col * P + (t * kTile & (P - 1)) + 8 * grp;
+    const E* p = static_cast<const E*>(a.vc) + head_at(page) + (t * kTile & (P - 1));
 #pragma unroll
-    for (int v = 0; v < NV; v++) vf[v] = *reinterpret_cast<const u32x4*>(p + off + 16 * v * P);
+    for (int v = 0; v < NV; v++) vf[v] = *reinterpret_cast<const u32x4*>(p + 16 * v * P + v_off);
   };
 
+  uint32_t odd = 0;   // not 0: this wave left values out that are not finite
   // One tile: scores, softmax state, and the second product.  EDGE: slots that not
   // everybody sees are among the tile's (drafts, or none at all).
-  auto step = [&](auto edge_c, const u32x4 (&kf)[2][NC], u32x4 (&vf)[NV], int page, int t) {
+  // get_k and get_v give the tile's operands, from registers or LDS.
+  auto step = [&](auto edge_c, auto get_k, auto get_v, int t) {
     constexpr bool EDGE = decltype(edge_c)::value;
     const int j0 = t * kTile + 8 * grp;
     f32x4 sc[RT][2];
 #pragma unroll
-    for (int rt = 0; rt < RT; rt++)
+    for (int kt = 0; kt < 2; kt++)
 #pragma unroll
-      for (int kt = 0; kt < 2; kt++) {
-        f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int c = 0; c < NC; c++) {
+        const u32x4 k = get_k(kt, c);
 #pragma unroll
-        for (int c = 0; c < NC; c++) x = product<TYPE>(kf[kt][c], qf[rt][c], x);
-        sc[rt][kt] = x;
+        for (int rt = 0; rt < RT; rt++) sc[rt][kt] = product<TYPE>(k, qf[rt][c], c ? sc[rt][kt] : f32x4{0.f, 0.f, 0.f, 0.f});
       }
-    uint32_t odd = 0;     // this lane's keys with a value that is not finite
-    if constexpr (EDGE) {
-      const int valid = min(max(total - j0, 0), 8);
-      uint32_t in[4];
-#pragma unroll
-      for (int i = 0; i < 4; i++) in[i] = valid >= 2 * i + 2 ? 0xFFFFFFFFu : (valid == 2 * i + 1 ? 0xFFFFu : 0u);
-#pragma unroll
-      for (int v = 0; v < NV; v++)
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-          const uint32_t bad = not_finite<TYPE>(vf[v][i]) & in[i];
-          vf[v][i] &= in[i] & ~bad;
-          odd |= (bad & 1u) << 2 * i | (bad >> 31) << (2 * i + 1);
-        }
-    }
     u32x4 pf[RT];
-    uint32_t see[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; rt++) {
-      float x[8];
+      float x[8], y[8];
+      uint32_t see = 0xFFu;
+      if constexpr (EDGE) see = seen8(a, q.off + tok[rt], tok[rt], q.n, j0 - q.len);
 #pragma unroll
-      for (int e = 0; e < 8; e++) x[e] = sc[rt][e >> 2][e & 3] * a.scale2;
-      if constexpr (EDGE) {
-        see[rt] = seen8(a, q.off + tok[rt], tok[rt], q.n, j0 - q.len);
-#pragma unroll
-        for (int e = 0; e < 8; e++) x[e] = see[rt] >> e & 1 ? x[e] : -INFINITY;
+      for (int e = 0; e < 8; e++) {
+        x[e] = sc[rt][e >> 2][e & 3];
+        if constexpr (EDGE) x[e] = see >> e & 1 ? x[e] : -INFINITY;
+        y[e] = __fmaf_rn(x[e], a.scale2, -ms[rt]);
       }
-      float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-      mx = rows_max(mx);
-      const float m2 = fmaxf(m[rt], mx), ms = m2 == -INFINITY ? 0.f : m2;
-      if (__any(m2 > m[rt])) {
-        const float f = __builtin_amdgcn_exp2f(m[rt] - ms);
+      auto most = [](const float (&v)[8]) {
+        return fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
+      };
+      // A row's maximum moves only when a score passes it by kSlack: until then weights
+      // stay below 2^kSlack, and no lane asks the others for theirs.  (A row that has seen
+      // nothing has -infinity, which any score passes.)
+      if (__any(!(most(y) <= kSlack))) {
+        const bool moves = !(rows_max(most(y)) <= kSlack);    // this row, whatever its neighbours do
+        const float m2 = moves ? fmaxf(m[rt], rows_max(most(x))) : m[rt];
+        const float ms2 = m2 == -INFINITY ? 0.f : m2 * a.scale2;
+        const float f = m[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms[rt] - ms2);
         l[rt] *= f;
 #pragma unroll
         for (int v = 0; v < NV; v++)
 #pragma unroll
           for (int i = 0; i < 4; i++) o[rt][v][i] *= f;
         m[rt] = m2;
+        ms[rt] = m2 == -INFINITY ? -INFINITY : ms2;
+#pragma unroll
+        for (int e = 0; e < 8; e++) y[e] = __fmaf_rn(x[e], a.scale2, -ms2);
       }
       float p[8];
 #pragma unroll
-      for (int e = 0; e < 8; e++) p[e] = __builtin_amdgcn_exp2f(x[e] - ms);
+      for (int e = 0; e < 8; e++) {
+        p[e] = __builtin_amdgcn_exp2f(y[e]);
+        if constexpr (EDGE) p[e] = see >> e & 1 ? p[e] : 0.f;
+      }
       l[rt] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
       pf[rt] = u32x4{pack2<TYPE>(p[0], p[1]), pack2<TYPE>(p[2], p[3]), pack2<TYPE>(p[4], p[5]), pack2<TYPE>(p[6], p[7])};
     }
+    const int valid = min(max(total - j0, 0), 8);
 #pragma unroll
-    for (int v = 0; v < NV; v++)
+    for (int v = 0; v < NV; v++) {
+      u32x4 w = get_v(v);
+      if constexpr (EDGE)
 #pragma unroll
-      for (int rt = 0; rt < RT; rt++) o[rt][v] = product<TYPE>(vf[v], pf[rt], o[rt][v]);
-    if constexpr (EDGE) {
-      if (!__any(odd != 0)) return;
-      // Infinite and NaN values left the product, where 0 * NaN would reach the rows that
-      // do not see them; here they go to the rows that do.
-      const E* vp = static_cast<const E*>(a.vc) + head_at(page) + (t * kTile & (P - 1)) + 4 * grp * P;
+        for (int i = 0; i < 4; i++) {   // slots past the last token, and what is not finite, as zeros
+          const uint32_t in = valid >= 2 * i + 2 ? 0xFFFFFFFFu : (valid == 2 * i + 1 ? 0xFFFFu : 0u);
+          const uint32_t bad = not_finite<TYPE>(w[i]) & in;
+          w[i] &= in & ~bad;
+          odd |= bad;
+        }
+#pragma unroll
+      for (int rt = 0; rt < RT; rt++) o[rt][v] = product<TYPE>(w, pf[rt], o[rt][v]);
+    }
+  };
+
+  const int t_full = min(t_end, q.len / kTile);    // tiles before it hold cached tokens alone
+  if constexpr (RW == 1) {
+    // the next tile's keys load behind this one's products; tiles with drafts in them, the
+    // last ones, go one at a time
+    int n = 0, t = t_first + wk;
+    auto next_page = [&]() {
+      if (++n % kWave == 0) look_up(n);
+      return static_cast<int>(__builtin_amdgcn_readlane(pages, n % kWave));
+    };
+    look_up(0);
+    int page = __builtin_amdgcn_readfirstlane(pages);
+    if (t < t_full) {
+      u32x4 kf[2][NC], vf[NV], kn[2][NC];
+      load_k(kf, page, t);
+      for (; t < t_full; t += KW) {
+        load_v(vf, page, t);
+        const int next = next_page();
+        if (t + KW < t_full) load_k(kn, next, t + KW);
+        if (page >= 0)
+          step(std::false_type{}, [&](int kt, int c) { return kf[kt][c]; }, [&](int v) { return vf[v]; }, t);
+#pragma unroll
+        for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+          for (int c = 0; c < NC; c++) kf[kt][c] = kn[kt][c];
+        page = next;
+      }
+    }
 #pragma unroll 1
-      for (int key = 0; key < kTile; key++) {
-        if (!__any(grp == key >> 3 && (odd >> (key & 7) & 1))) continue;
+    for (; t < t_end; t += KW) {
+      if (page >= 0) {
+        u32x4 kf[2][NC], vf[NV];
+        load_k(kf, page, t);
+        load_v(vf, page, t);
+        step(std::true_type{}, [&](int kt, int c) { return kf[kt][c]; }, [&](int v) { return vf[v]; }, t);
+      }
+      page = next_page();
+    }
+  } else {
+    Lds& lds = *reinterpret_cast<Lds*>(lds_bytes);
+    const int tid = threadIdx.x % TG, wtid = wr * kWave;
+    u32x4 kp[NP], vp[NP];
+    // loads of stage r; bit j of the answer: its j-th tile is there
+    auto load = [&](int r) {
+      if (r * KT % kWave == 0) look_up(r * KT);
+      uint32_t there = 0;
 #pragma unroll
-        for (int rt = 0; rt < RT; rt++) {
-          uint32_t w = pf[rt][0];
+      for (int j = 0; j < KT; j++) {
+        const int t = tile_of(r * KT + j), page = __builtin_amdgcn_readlane(pages, (r * KT + j) % kWave);
+        if (t >= t_end || page < 0) continue;
+        there |= 1u << j;
+        const E *kb = static_cast<const E*>(a.kc) + head_at(page) + (t * kTile & (P - 1)) * D;
+        const E *vb = static_cast<const E*>(a.vc) + head_at(page) + (t * kTile & (P - 1));
 #pragma unroll
-          for (int i = 1; i < 4; i++) w = (key & 7) >> 1 == i ? pf[rt][i] : w;
-          w = __shfl(w, 16 * (key >> 3) + col);
-          const float p = key & 1 ? half_hi<TYPE>(w) : half_lo<TYPE>(w);
-          const bool sees = __shfl(see[rt], 16 * (key >> 3) + col) >> (key & 7) & 1;
+        for (int i = 0; i < NP; i++) {
+          if ((wtid + i * TG) / (4 * D) != j) continue;     // the same for a whole wave
+          const uint32_t x = (tid + i * TG) % (4 * D);
+          kp[i] = *reinterpret_cast<const u32x4*>(kb + x * 8);
+          vp[i] = *reinterpret_cast<const u32x4*>(vb + ((x >> 2) * P + (x & 3) * 8));
+        }
+      }
+      return there;
+    };
+    uint32_t there = load(0);
+    auto stage = [&](auto edge_c, int r) {
+      Tile (&tiles_r)[KT] = lds.tile[r & 1][wk];
+#pragma unroll
+      for (int i = 0; i < NP; i++) {
+        Tile& tile = tiles_r[(wtid + i * TG) / (4 * D)];
+        const int x = (tid + i * TG) % (4 * D), key = x / (D / 8), row = 16 * (key >> 2 & 1) + 4 * (key >> 3) + (key & 3);
+        tile.k[row][x % (D / 8) ^ (D == 64 ? row >> 1 & 7 : row & 15)] = kp[i];
+        tile.v[x >> 2][(x & 3) ^ (x >> 4 & 3)] = vp[i];
+      }
+      const uint32_t now = there;
+      __syncthreads();
+      there = load(r + 1);
+#pragma unroll 1
+      for (int j = 0; j < KT; j++) {
+        const Tile& tile = tiles_r[j];
+        if (now >> j & 1)
+          step(edge_c, [&](int kt, int c) { return tile.k[16 * kt + col][(4 * c + grp) ^ (D == 64 ? col >> 1 : col)]; },
+               [&](int v) { return tile.v[16 * v + col][grp ^ (col >> 2)]; }, tile_of(r * KT + j));
+      }
+    };
+    const int stages = (t_end - t_first + KW * KT - 1) / (KW * KT), full = max(0, t_full - t_first) / (KW * KT);
+    for (int r = 0; r < full; r++) stage(std::false_type{}, r);
+#pragma unroll 1
+    for (int r = full; r < stages; r++) stage(std::true_type{}, r);
+    __syncthreads();    // the tiles' place is taken by the sums
+  }
+
+  if (__any(odd != 0)) {
+    // Infinite and NaN values of drafts were left out of the products, where 0 * NaN would
+    // have reached the rows that do not see them; here they go to the rows that do.
+#pragma unroll 1
+    for (int n = 0; n < (t_end - t_first + KW * KT - 1) / (KW * KT) * KT; n++) {
+      const int tf = tile_of(n);
+      if (tf < t_full || tf >= t_end) continue;
+      const int pg = __builtin_amdgcn_readfirstlane(page_of(a.b, s, tf * kTile));
+      if (pg < 0) continue;
+      const E* kb = static_cast<const E*>(a.kc) + head_at(pg) + (tf * kTile & (P - 1)) * D;
+      const E* vb = static_cast<const E*>(a.vc) + head_at(pg) + (tf * kTile & (P - 1));
+#pragma unroll
+      for (int rt = 0; rt < RT; rt++)
+#pragma unroll 1
+        for (int key = 0; key < min(kTile, total - tf * kTile); key++) {
+          // the score of this lane's row and the key, from the four lanes that hold the row
+          float x = 0.f;
+#pragma unroll 1
+          for (int c = 0; c < NC; c++) {
+            u32x4 qc = qf[rt][0];
+#pragma unroll
+            for (int i = 1; i < NC; i++) qc = c == i ? qf[rt][i] : qc;
+            const u32x4 k = *reinterpret_cast<const u32x4*>(kb + key * D + 32 * c + 8 * grp);
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+              x += half_lo<TYPE>(qc[i]) * half_lo<TYPE>(k[i]) + half_hi<TYPE>(qc[i]) * half_hi<TYPE>(k[i]);
+          }
+          x = rows_sum(x);
+          const bool sees = seen8(a, q.off + tok[rt], tok[rt], q.n, tf * kTile + key - q.len) & 1;
+          const float p = __builtin_amdgcn_exp2f(__fmaf_rn(x, a.scale2, m[rt] == -INFINITY ? 0.f : -(m[rt] * a.scale2)));
 #pragma unroll
           for (int v = 0; v < NV; v++)
 #pragma unroll
             for (int i = 0; i < 4; i++) {
-              const float x = static_cast<float>(vp[(16 * v + i) * P + key]);
-              o[rt][v][i] += __builtin_isfinite(x) || !sees ? 0.f : p * x;
+              const float val = static_cast<float>((vb + key + (16 * v + i) * P)[o_off]);
+              if (!__builtin_isfinite(val) && sees) o[rt][v][i] += p * val;
+              __builtin_amdgcn_sched_barrier(0);   // one load at a time: registers for a rare case
             }
         }
-      }
-    }
-  };
-
-  // Tiles whose slots all hold cached tokens come first, the next tile's keys loading
-  // behind this one's products; the last ones, with drafts in them, one at a time.
-  const int t_full = min(t_end, q.len / kTile);
-  int left = 0, t = t_begin;
-  if (t < t_end) look_up(t);
-  if (t < t_full) {
-    u32x4 kf[2][NC], vf[NV], kn[2][NC];
-    int page = __builtin_amdgcn_readfirstlane(pages);
-    load_k(kf, page, t);
-    for (; t < t_full; t += key_waves) {
-      load_v(vf, page, t);
-      if (++left == kWave) {
-        look_up(t + key_waves);
-        left = 0;
-      }
-      const int next = __builtin_amdgcn_readlane(pages, left);
-      if (t + key_waves < t_full) load_k(kn, next, t + key_waves);
-      if (page >= 0) step(std::false_type{}, kf, vf, page, t);
-#pragma unroll
-      for (int kt = 0; kt < 2; kt++)
-#pragma unroll
-        for (int c = 0; c < NC; c++) kf[kt][c] = kn[kt][c];
-      page = next;
     }
   }
-#pragma unroll 1
-  for (; t < t_end; t += key_waves) {
-    const int page = __builtin_amdgcn_readlane(pages, left);
-    if (page >= 0) {
-      u32x4 kf[2][NC], vf[NV];
-      load_k(kf, page, t);
-      load_v(vf, page, t);
-      step(std::true_type{}, kf, vf, page, t);
-    }
-    if (++left == kWave) {
-      look_up(t + key_waves);
-      left = 0;
-    }
-  }
+  Sums& sums = *reinterpret_cast<Sums*>(lds_bytes);
 
   // join the waves that shared the rows: common maximum, then the sums in wave order
 #pragma unroll
@@ -285,28 +394,28 @@ __global__ void __launch_bounds__(kWaves * kWave, D * RT <= 256 ? 2 : 1) attend_
 #pragma unroll
   for (int rt = 0; rt < RT; rt++) {
     float top = -INFINITY;
-    for (int w = 0; w < key_waves; w++) top = fmaxf(top, stats[w * a.rows_wave + wr][rt][col][0]);
-    const float f = m[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[rt] - top);
+    for (int w = 0; w < KW; w++) top = fmaxf(top, stats[w * RW + wr][rt][col][0]);
+    const float f = m[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[rt] - top) * a.scale2);
     if (rt) __syncthreads();
 #pragma unroll
     for (int v = 0; v < NV; v++) {
       f32x4 x = o[rt][v];
 #pragma unroll
       for (int i = 0; i < 4; i++) x[i] *= f;
-      *reinterpret_cast<f32x4*>(&sums[wave][col][16 * v + 4 * grp]) = x;
+      *reinterpret_cast<f32x4*>(&sums.x[wave][col][16 * v + 4 * grp]) = x;
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < a.rows_wave * 16 * (D / 4); i += kWaves * kWave) {
+    for (int i = threadIdx.x; i < RW * 16 * (D / 4); i += W * kWave) {
       const int c = i % (D / 4) * 4, rr = i / (D / 4) % 16, w0 = i / (D / 4) / 16;
       const int r = row0 + (w0 * RT + rt) * 16 + rr;
       if (r >= rows) continue;
       float hi = -INFINITY, sum = 0.f;
-      for (int w = 0; w < key_waves; w++) hi = fmaxf(hi, stats[w * a.rows_wave + w0][rt][rr][0]);
+      for (int w = 0; w < KW; w++) hi = fmaxf(hi, stats[w * RW + w0][rt][rr][0]);
       f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
-      for (int w = 0; w < key_waves; w++) {
-        const float mw = stats[w * a.rows_wave + w0][rt][rr][0];
-        if (mw != -INFINITY) sum += stats[w * a.rows_wave + w0][rt][rr][1] * __builtin_amdgcn_exp2f(mw - hi);
-        const f32x4 y = *reinterpret_cast<const f32x4*>(&sums[w * a.rows_wave + w0][rr][c]);
+      for (int w = 0; w < KW; w++) {
+        const float mw = stats[w * RW + w0][rt][rr][0];
+        if (mw != -INFINITY) sum += stats[w * RW + w0][rt][rr][1] * __builtin_amdgcn_exp2f((mw - hi) * a.scale2);
+        const f32x4 y = *reinterpret_cast<const f32x4*>(&sums.x[w * RW + w0][rr][c]);
 #pragma unroll
         for (int e = 0; e < 4; e++) x[e] += y[e];
       }
@@ -328,13 +437,16 @@ __global__ void __launch_bounds__(kWaves * kWave, D * RT <= 256 ? 2 : 1) attend_
   }
 }
 
-// One wave per (new token, query head): joins its parts in order.
-template <int TYPE, int D>
+// Joins the parts of each (new token, query head): WPR waves take every WPR-th part, lanes
+// side by side over the channels, and are added in wave order.
+template <int TYPE, int D, int WPR>
 __global__ void __launch_bounds__(256) join_kernel(AttendArgs a) {
   typedef elem_t<TYPE> E;
+  constexpr int C = D / kWave, U = 4;   // U parts' loads at once
+  __shared__ float sums[4][D];
   const int64_t all_rows = static_cast<int64_t>(a.b.n_seqs) * a.b.max_new * a.n_q_heads;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t row = WPR == 4 ? blockIdx.x : static_cast<int64_t>(blockIdx.x) * 4 + wave;
   if (row >= all_rows) return;
   const int head = static_cast<int>(row % a.n_q_heads);
   const int64_t tok = row / a.n_q_heads;
@@ -342,62 +454,96 @@ __global__ void __launch_bounds__(256) join_kernel(AttendArgs a) {
   bool ok;
   const Seq q = sequence(a.b, s, ok);
   if (i >= q.n) return;
-  const int tiles = (q.len + q.n + kTile - 1) / kTile, per = tiles_per_part(tiles, a.n_split);
+  const int tiles = (q.len + q.n + kTile - 1) / kTile, per = tiles_per_part(a, tiles);
   const int parts = (tiles + per - 1) / per;
   float m = -INFINITY, l = 0.f;
   if (lane < parts) {
     m = a.stat[2 * (lane * all_rows + row)];
     l = a.stat[2 * (lane * all_rows + row) + 1];
   }
+  float x[C];
+#pragma unroll
+  for (int c = 0; c < C; c++) x[c] = 0.f;
   float top = m;
   for (int w = 32; w; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
-  const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-  float sum = l * f;
-  for (int w = 32; w; w >>= 1) sum += __shfl_xor(sum, w);
+  const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * a.scale2);
+  const float sum = wave_sum(l * f);
   const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-  float x[D / kWave];
+  for (int p0 = WPR == 4 ? wave : 0; p0 < parts; p0 += WPR * U) {
+    float y[U][C];
 #pragma unroll
-  for (int c = 0; c < D / kWave; c++) x[c] = 0.f;
-  for (int p = 0; p < parts; p++) {
-    const float fp = __shfl(f, p);
+    for (int u = 0; u < U; u++)
 #pragma unroll
-    for (int c = 0; c < D / kWave; c++) x[c] = __fmaf_rn(fp, a.part[(p * all_rows + row) * D + lane * (D / kWave) + c], x[c]);
+      for (int c = 0; c < C; c++) y[u][c] = p0 + WPR * u < parts ? a.part[((p0 + WPR * u) * all_rows + row) * D + lane * C + c] : 0.f;
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const float fp = __shfl(f, (p0 + WPR * u) & 63);
+#pragma unroll
+      for (int c = 0; c < C; c++) x[c] = p0 + WPR * u < parts ? __fmaf_rn(fp, y[u][c], x[c]) : x[c];
+    }
   }
-  E* op = static_cast<E*>(a.out) + (q.off + i) * a.ld_out + head * D + lane * (D / kWave);
+  E* op = static_cast<E*>(a.out) + (q.off + i) * a.ld_out + head * D;
+  if constexpr (WPR == 1) {
 #pragma unroll
-  for (int c = 0; c < D / kWave; c++) op[c] = static_cast<E>(x[c] * inv);
+    for (int c = 0; c < C; c++) op[lane * C + c] = static_cast<E>(x[c] * inv);
+  } else {
+#pragma unroll
+    for (int c = 0; c < C; c++) sums[wave][lane * C + c] = x[c];
+    __syncthreads();
+    const int c = threadIdx.x;
+    if (c < D) op[c] = static_cast<E>((((sums[0][c] + sums[1][c]) + sums[2][c]) + sums[3][c]) * inv);
+  }
 }
 
-// How a batch is laid over workgroups.
+// How a batch is laid over workgroups.  Up to 16 rows (32 where the registers allow two
+// tiles) per key head go straight from memory, more through LDS with as many row waves as
+// it takes.  Parts: enough for 1024 workgroups straight from memory (four a CU), 256 through LDS
+// (one a CU; with 512, which run one after another, the large trees take 190 us instead
+// of 174, 2 x 32 drafts over 16000 51 instead of 40, 4 x 12 of head_dim 256 over 4000 30
+// instead of 20), and no shorter than two steps of every wave.
 struct Plan {
+  int row_waves;   // RW of the kernel
   int row_tiles;   // 16-row tiles of a wave
-  int rows_wave;   // waves of a workgroup that take other rows; the rest take other keys
   int row_blocks;  // workgroups over the rows
   int n_split;     // parts of the keys
+  int part_tiles;  // tiles of a part of the longest sequence
 };
 
 Plan plan_of(const moe_cache_t* C, int n_q_heads, int n_seqs, int max_new, int max_len) {
   const int64_t rows = static_cast<int64_t>(max_new) * (n_q_heads / C->n_heads);
+  const bool wide = C->head_dim == 256;
   Plan p;
-  p.row_tiles = rows <= 16 ? 1 : (rows <= 32 || C->head_dim == 256 ? 2 : 4);
-  p.rows_wave = 1;
-  while (p.rows_wave < kWaves && p.rows_wave * p.row_tiles * 16 < rows) p.rows_wave *= 2;
-  p.row_blocks = static_cast<int>(cdiv(rows, p.rows_wave * p.row_tiles * 16));
-  const int64_t wgs = static_cast<int64_t>(n_seqs) * C->n_heads * p.row_blocks;
-  const int64_t steps = cdiv(max_len, kTile * (kWaves / p.rows_wave));
-  p.n_split = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({cdiv(1024, std::max<int64_t>(wgs, 1)), steps / 2, kMaxSplit})));
+  p.row_tiles = wide || rows <= 16 ? 1 : 2;
+  p.row_waves = 1;
+  if (rows > 16 * p.row_tiles)
+    for (p.row_waves = wide ? 4 : 2; p.row_waves < 8 && p.row_waves * p.row_tiles * 16 < rows;) p.row_waves *= 2;
+  p.row_blocks = static_cast<int>(cdiv(rows, p.row_waves * p.row_tiles * 16));
+  const int key_waves = (p.row_waves == 1 ? 4 : 8) / p.row_waves;
+  const int64_t wgs = std::max<int64_t>(1, static_cast<int64_t>(n_seqs) * C->n_heads * p.row_blocks);
+  const int64_t tiles = std::max<int64_t>(1, cdiv(max_len, kTile));
+  const int64_t want = std::max<int64_t>(1, std::min<int64_t>({cdiv(p.row_waves == 1 ? 1024 : 256, wgs), tiles / (2 * key_waves), kMaxSplit}));
+  p.part_tiles = static_cast<int>(cdiv(tiles, want));
+  p.n_split = static_cast<int>(cdiv(tiles, p.part_tiles));
   return p;
 }
 
 template <int TYPE, int D>
 void launch(const Plan& p, hipStream_t s, const AttendArgs& a) {
-  const dim3 grid(static_cast<unsigned>(cdiv(a.units, 8) * 8 * p.row_blocks)), block(kWaves * kWave);
-  if (p.row_tiles == 1) hipLaunchKernelGGL((attend_kernel<TYPE, D, 1>), grid, block, 0, s, a);
-  else if (p.row_tiles == 2) hipLaunchKernelGGL((attend_kernel<TYPE, D, 2>), grid, block, 0, s, a);
-  else if constexpr (D < 256) hipLaunchKernelGGL((attend_kernel<TYPE, D, 4>), grid, block, 0, s, a);
+  const dim3 grid(static_cast<unsigned>(cdiv(a.units, 8) * 8 * p.row_blocks));
+  constexpr int RT = D == 256 ? 1 : 2;
+  if (p.row_waves == 1 && p.row_tiles == 1) hipLaunchKernelGGL((attend_kernel<TYPE, D, 1, 1>), grid, dim3(256), 0, s, a);
+  else if (p.row_waves == 4) hipLaunchKernelGGL((attend_kernel<TYPE, D, RT, 4>), grid, dim3(512), 0, s, a);
+  else if (p.row_waves == 8) hipLaunchKernelGGL((attend_kernel<TYPE, D, RT, 8>), grid, dim3(512), 0, s, a);
+  else if constexpr (D < 256) {
+    if (p.row_waves == 1) hipLaunchKernelGGL((attend_kernel<TYPE, D, 2, 1>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((attend_kernel<TYPE, D, 2, 2>), grid, dim3(512), 0, s, a);
+  }
   if (p.n_split > 1) {
     const int64_t rows = static_cast<int64_t>(a.b.n_seqs) * a.b.max_new * a.n_q_heads;
-    hipLaunchKernelGGL((join_kernel<TYPE, D>), dim3(static_cast<unsigned>(cdiv(rows, 4))), dim3(256), 0, s, a);
+    // few rows of many parts by a workgroup each, many rows by a wave (63 parts of 32 rows: 4.7
+    // us against 22; 8 of 8192: 18 against 9)
+    if (p.n_split > 16) hipLaunchKernelGGL((join_kernel<TYPE, D, 4>), dim3(static_cast<unsigned>(rows)), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((join_kernel<TYPE, D, 1>), dim3(static_cast<unsigned>(cdiv(rows, 4))), dim3(256), 0, s, a);
   }
 }
 
@@ -457,8 +603,8 @@ extern "C" int moe_tree_attention(const moe_cache_t* C, const int32_t* table, in
   float* part = static_cast<float*>(ws);
   const AttendArgs a{batch_of(C, table, max_pages, cache_len, n_seqs, new_off, n_tokens, max_new, status),
                      q, C->k, C->v, out, part, part + p.n_split * all_rows * C->head_dim, mask, ld_q, ld_out,
-                     scale * 1.44269504088896340736f, n_q_heads, n_q_heads / C->n_heads, mask_words, p.n_split,
-                     p.row_blocks, p.rows_wave, n_seqs * C->n_heads * p.n_split};
+                     __builtin_fabsf(scale) * 1.44269504088896340736f, scale < 0.f ? 0x80008000u : 0u, n_q_heads,
+                     n_q_heads / C->n_heads, mask_words, p.n_split, p.part_tiles, p.row_blocks, n_seqs * C->n_heads * p.n_split};
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (C->type == MOE_TYPE_BF16) launch<MOE_TYPE_BF16>(C->head_dim, p, s, a);
   else launch<MOE_TYPE_FP16>(C->head_dim, p, s, a);

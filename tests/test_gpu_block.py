@@ -429,8 +429,11 @@ def test_attend(lens, new, page, Hq, Hkv, D, dt, chain):
         other = cache.attend(q, off, max(new), guess, mask=mask, scale=scale)
         within(other, want, bound, "attend, another split")
     room = torch.full((N, Hq + 1, D), 5.0, device="cuda").to(dt)
-    cache.attend(q, off, max(new) + 3, max(a + n for a, n in zip(lens, new)), mask=mask, scale=scale, out=room[:, :Hq])
+    cache.attend(q, off, max(new), max(a + n for a, n in zip(lens, new)), mask=mask, scale=scale, out=room[:, :Hq])
     assert torch.equal(room[:, :Hq], out) and (room[:, Hq] == 5).all()
+    # a larger max_new than any sequence has lays the rows out differently
+    other = cache.attend(q, off, max(new) + 3, max(a + n for a, n in zip(lens, new)), mask=mask, scale=scale)
+    within(other, want, bound, "attend, another max_new")
 
 
 @pytest.mark.parametrize("big", [0.0, 30.0, -30.0])
