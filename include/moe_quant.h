@@ -660,7 +660,7 @@ int moe_tree_attention_plan(const moe_cache_t* C, int32_t n_q_heads, int32_t n_s
  *   ws        device workspace of moe_tree_attention_plan's bytes for the same
  *             sizes (NULL when that is 0); scratch between calls.
  * Scores, softmax and sums are fp32; the softmax weights enter the second
- * product rounded to the cache's type, as its matrix operand.  n_q_heads is a multiple of
+ * product and their own sum rounded to the cache's type, as a matrix operand.  n_q_heads is a multiple of
  * n_heads, at most 64 times it.  Results are bitwise reproducible.
  */
 int moe_tree_attention(const moe_cache_t* C, const int32_t* table, int32_t max_pages,

@@ -189,20 +189,22 @@ def _stream(stream, t: torch.Tensor) -> int:
     return torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else stream.cuda_stream
 
 
-def _rows(t: torch.Tensor, shape: tuple, what: str) -> int:
-    """Data pointer of a device tensor of this shape whose rows are contiguous."""
-    if t.shape == shape and t.is_cuda and (t.is_contiguous() or t.stride(-1) == 1 or shape[-1] <= 1):
-        return t.data_ptr()
-    raise MoEError("%s must be a device tensor of shape %s with contiguous rows" % (what, tuple(shape)))
+def _rows(t: torch.Tensor, T: int, n: int, what: str) -> Tuple[int, int]:
+    """(data pointer, row stride) of a [T][n] device tensor whose rows are contiguous."""
+    if t.shape == (T, n) and t.is_cuda:
+        s = t.stride()
+        if s[1] == 1 or n <= 1:
+            return t.data_ptr(), s[0] if T > 1 else n
+    raise MoEError("%s must be a device tensor of shape (%d, %d) with contiguous rows" % (what, T, n))
 
 
 def _flat(t: Optional[torch.Tensor], shape: tuple, dtype: torch.dtype, what: str):
     """Data pointer of a contiguous device tensor (None for None)."""
     if t is None:
         return None
-    if t.dtype != dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
-        raise MoEError("%s must be a contiguous %s device tensor of shape %s" % (what, dtype, tuple(shape)))
-    return t.data_ptr()
+    if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    raise MoEError("%s must be a contiguous %s device tensor of shape %s" % (what, dtype, tuple(shape)))
 
 
 def moe_quant_linear(x: torch.Tensor, codes: torch.Tensor, sz: torch.Tensor, y: torch.Tensor,
@@ -217,17 +219,20 @@ def moe_quant_linear(x: torch.Tensor, codes: torch.Tensor, sz: torch.Tensor, y: 
     G, R = sz.shape
     if G < 1 or K % G:
         raise MoEError("sz has %d groups for K = %d" % (G, K))
-    if codes.dtype != torch.int32 or sz.dtype != torch.int32 or not sz.is_cuda:
+    if codes.dtype is not torch.int32 or sz.dtype is not torch.int32 or not sz.is_cuda:
         raise MoEError("codes and sz must be int32 device tensors")
-    if codes.dim() != 2 or codes.shape[0] != R or codes.shape[1] * 8 < K:
+    words = codes.shape[-1]
+    if words * 8 < K:
         raise MoEError("codes have shape %s for %d rows of K = %d" % (tuple(codes.shape), R, K))
-    st = load().moe_quant_linear(_rows(x, (T, K), "x"), _type(x, "x"), x.stride(0) if T > 1 else K, T, K,
-                                 _rows(codes, codes.shape, "codes"), codes.stride(0) if R > 1 else codes.shape[1],
-                                 sz.data_ptr(), sz.stride(1) if R > 1 else 1, sz.stride(0) if G > 1 else R,
-                                 R, bits, K // G, _flat(bias, (R,), torch.float32, "bias"),
-                                 _rows(y, (T, R), "y"), _type(y, "y"), y.stride(0) if T > 1 else R,
-                                 _stream(stream, x))
-    check(st, "moe_quant_linear")
+    sg, sr = sz.stride()
+    xp, ld_x = _rows(x, T, K, "x")
+    cp, ld_c = _rows(codes, R, words, "codes")
+    yp, ld_y = _rows(y, T, R, "y")
+    st = load().moe_quant_linear(xp, _type(x, "x"), ld_x, T, K, cp, ld_c, sz.data_ptr(), sr if R > 1 else 1,
+                                 sg if G > 1 else R, R, bits, K // G, _flat(bias, (R,), torch.float32, "bias"),
+                                 yp, _type(y, "y"), ld_y, _stream(stream, x))
+    if st:
+        check(st, "moe_quant_linear")
 
 
 def moe_block_norm(r: torch.Tensor, h: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
@@ -242,41 +247,43 @@ def moe_block_norm(r: torch.Tensor, h: Optional[torch.Tensor] = None, y: Optiona
     residual alone; without w_post, y is taken as it is.  r_out may be r, h may be r or y.
     """
     T, d = r.shape
-    one = T == 1
     g, g_type, g_row, g_col = None, 0, 0, 0
     if gate is not None:
         g_type = _type(gate, "gate")
         if gate.dim() == 1:
-            g, g_col = _rows(gate, (d,), "gate"), 1
-        elif gate.dim() == 2 and gate.shape[1] == 1 and d > 1:
-            g, g_row = _rows(gate, (T, 1), "gate"), 0 if one else gate.stride(0)
+            g, g_col = _rows(gate[None], 1, d, "gate")[0], 1
+        elif gate.shape[1] == 1 and d > 1:
+            g, g_row = _rows(gate, T, 1, "gate")
         else:
-            g, g_row, g_col = _rows(gate, (T, d), "gate"), 0 if one else gate.stride(0), 1
-    if r_out is not None and r_out.dtype != r.dtype:
-        raise MoEError("r_out must have the type of r")
-    st = load().moe_block_norm(
-        None if y is None else _rows(y, (T, d), "y"), 0 if y is None else _type(y, "y"),
-        d if y is None or one else y.stride(0),
-        _rows(r, (T, d), "r"), _type(r, "r"), d if one else r.stride(0), T, d,
-        _flat(w_post, (d,), torch.float32, "w_post"), g, g_type, g_row, g_col, branch_scale, residual_scale,
-        _flat(w_pre, (d,), torch.float32, "w_pre"), eps,
-        None if r_out is None else _rows(r_out, (T, d), "r_out"), d if r_out is None or one else r_out.stride(0),
-        None if h is None else _rows(h, (T, d), "h"), 0 if h is None else _type(h, "h"),
-        d if h is None or one else h.stride(0), _stream(stream, r))
-    check(st, "moe_block_norm")
+            (g, g_row), g_col = _rows(gate, T, d, "gate"), 1
+    yp, ld_y, y_type = None, d, 0
+    if y is not None:
+        (yp, ld_y), y_type = _rows(y, T, d, "y"), _type(y, "y")
+    op, ld_o = None, d
+    if r_out is not None:
+        if r_out.dtype is not r.dtype:
+            raise MoEError("r_out must have the type of r")
+        op, ld_o = _rows(r_out, T, d, "r_out")
+    hp, ld_h, h_type = None, d, 0
+    if h is not None:
+        (hp, ld_h), h_type = _rows(h, T, d, "h"), _type(h, "h")
+    rp, ld_r = _rows(r, T, d, "r")
+    st = load().moe_block_norm(yp, y_type, ld_y, rp, _type(r, "r"), ld_r, T, d,
+                               _flat(w_post, (d,), torch.float32, "w_post"), g, g_type, g_row, g_col, branch_scale,
+                               residual_scale, _flat(w_pre, (d,), torch.float32, "w_pre"), eps, op, ld_o, hp, h_type,
+                               ld_h, _stream(stream, r))
+    if st:
+        check(st, "moe_block_norm")
 
 
-def _heads(t: torch.Tensor, shape: tuple, dtype: torch.dtype, what: str) -> int:
-    """Data pointer of a [tokens][heads][head_dim] device tensor whose heads lie side by side."""
-    if t.shape != shape or t.dtype != dtype or not t.is_cuda:
-        raise MoEError("%s must be a %s device tensor of shape %s" % (what, dtype, tuple(shape)))
-    if t.stride(2) != 1 or (shape[1] > 1 and t.stride(1) != shape[2]):
-        raise MoEError("the heads of a token of %s must lie side by side" % what)
-    return t.data_ptr()
-
-
-def _ld(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+def _heads(t: torch.Tensor, N: int, H: int, D: int, dtype: torch.dtype, what: str) -> Tuple[int, int]:
+    """(data pointer, token stride) of a [N][H][D] device tensor whose heads lie side by side."""
+    if t.dtype is dtype and t.shape == (N, H, D) and t.is_cuda:
+        s = t.stride()
+        if s[2] == 1 and (s[1] == D or H <= 1):
+            return t.data_ptr(), s[0] if N > 1 else H * D
+    raise MoEError("%s must be a %s device tensor of shape (%d, %d, %d), the heads of a token side by side"
+                   % (what, dtype, N, H, D))
 
 
 def _batch(table: torch.Tensor, lens: torch.Tensor, new_off: torch.Tensor):
@@ -298,21 +305,24 @@ def moe_cache_append(desc: CacheDesc, table: torch.Tensor, lens: torch.Tensor, n
                      interleaved: bool = False, status: Optional[torch.Tensor] = None, stream=None) -> None:
     """Rotate q and k [tokens][heads][head_dim] by cos/sin [max_pos][rot_dim/2] and store
     k and v of the new tokens in the cache."""
-    N, dt, D = k.shape[0], _DTYPE16[desc.type], desc.head_dim
-    kv = (N, desc.n_heads, D)
-    Hq = 0 if q is None else q.shape[1]
+    N, dt, D, Hkv = k.shape[0], _DTYPE16[desc.type], desc.head_dim, desc.n_heads
     if (q is None) != (q_out is None) or (cos is None) != (sin is None):
         raise MoEError("q and q_out, cos and sin come in pairs")
     tab = (1, 0) if cos is None else tuple(cos.shape)
+    qp, ld_q, Hq, op, ld_o = None, 0, 0, None, 0
+    if q is not None:
+        Hq = q.shape[1]
+        qp, ld_q = _heads(q, N, Hq, D, dt, "q")
+        op, ld_o = _heads(q_out, N, Hq, D, dt, "q_out")
+    kp, ld_k = _heads(k, N, Hkv, D, dt, "k")
+    vp, ld_v = _heads(v, N, Hkv, D, dt, "v")
     st = load().moe_cache_append(
-        C.byref(desc), *_batch(table, lens, new_off), N, max_new,
-        None if q is None else _heads(q, (N, Hq, D), dt, "q"), 0 if q is None else _ld(q), Hq,
-        _heads(k, kv, dt, "k"), _ld(k), _heads(v, kv, dt, "v"), _ld(v),
+        C.byref(desc), *_batch(table, lens, new_off), N, max_new, qp, ld_q, Hq, kp, ld_k, vp, ld_v,
         _flat(positions, (N,), torch.int32, "positions"), _flat(cos, tab, torch.float32, "cos"),
-        _flat(sin, tab, torch.float32, "sin"), 2 * tab[1], tab[0], int(interleaved),
-        None if q is None else _heads(q_out, (N, Hq, D), dt, "q_out"), 0 if q is None else _ld(q_out),
+        _flat(sin, tab, torch.float32, "sin"), 2 * tab[1], tab[0], int(interleaved), op, ld_o,
         _flat(status, (1,), torch.int32, "status"), _stream(stream, k))
-    check(st, "moe_cache_append")
+    if st:
+        check(st, "moe_cache_append")
 
 
 def moe_tree_attention_plan(desc: CacheDesc, n_q_heads: int, n_seqs: int, max_new: int,
@@ -332,17 +342,23 @@ def moe_tree_attention(desc: CacheDesc, table: torch.Tensor, lens: torch.Tensor,
     int64 [tokens][words]: bit m of a token's words, m % 64 of word m // 64, lets it see
     its sequence's new token m; None is a chain (each token sees itself and those before)."""
     N, Hq, D = q.shape
+    if D != desc.head_dim:
+        raise MoEError("q has heads of %d, the cache of %d" % (D, desc.head_dim))
     dt = _DTYPE16[desc.type]
     words = 0 if mask is None else mask.shape[-1]
-    if ws is not None and (not ws.is_cuda or not ws.is_contiguous()):
-        raise MoEError("ws must be a contiguous device tensor")
+    qp, ld_q = _heads(q, N, Hq, D, dt, "q")
+    op, ld_o = _heads(out, N, Hq, D, dt, "out")
+    wp, wb = None, 0
+    if ws is not None:
+        if not ws.is_cuda or not ws.is_contiguous():
+            raise MoEError("ws must be a contiguous device tensor")
+        wp, wb = ws.data_ptr(), ws.numel() * ws.element_size()
     st = load().moe_tree_attention(
-        C.byref(desc), *_batch(table, lens, new_off), N, max_new, max_len,
-        _heads(q, (N, Hq, desc.head_dim), dt, "q"), _ld(q), Hq, _flat(mask, (N, words), torch.int64, "mask"),
-        words, scale, _heads(out, (N, Hq, D), dt, "out"), _ld(out), _flat(status, (1,), torch.int32, "status"),
-        None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel() * ws.element_size(),
-        _stream(stream, q))
-    check(st, "moe_tree_attention")
+        C.byref(desc), *_batch(table, lens, new_off), N, max_new, max_len, qp, ld_q, Hq,
+        _flat(mask, (N, words), torch.int64, "mask"), words, scale, op, ld_o,
+        _flat(status, (1,), torch.int32, "status"), wp, wb, _stream(stream, q))
+    if st:
+        check(st, "moe_tree_attention")
 
 
 def moe_cache_keep(desc: CacheDesc, table: torch.Tensor, lens: torch.Tensor, new_off: torch.Tensor,
@@ -355,7 +371,8 @@ def moe_cache_keep(desc: CacheDesc, table: torch.Tensor, lens: torch.Tensor, new
         C.byref(desc), *_batch(table, lens, new_off), _flat(keep, (B, keep.shape[-1]), torch.int32, "keep"),
         keep.shape[-1], _flat(n_keep, (B,), torch.int32, "n_keep"), _flat(len_out, (B,), torch.int32, "len_out"),
         _flat(status, (1,), torch.int32, "status"), _stream(stream, lens))
-    check(st, "moe_cache_keep")
+    if st:
+        check(st, "moe_cache_keep")
 
 
 # ---------------------------------------------------------------------------

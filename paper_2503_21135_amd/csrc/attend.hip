@@ -10,6 +10,7 @@
 // keys takes keys 8*(r/4) + 4*kt + r%4 as its row r, which leaves lane group g = lane / 16
 // with the keys 8g .. 8g+7 in order.  K rows and (transposed) V rows are read from
 // memory straight into operands, 16 bytes a lane, with no pass through LDS.
+#include <algorithm>
 #include <type_traits>
 
 #include "cache.hpp"
@@ -39,12 +40,6 @@ struct AttendArgs {
 __device__ __forceinline__ int tiles_per_part(const AttendArgs& a, int tiles) {
   const int parts = min(a.n_split, (tiles + a.part_tiles - 1) / a.part_tiles);
   return (tiles + parts - 1) / max(parts, 1);
-}
-
-template <int TYPE>
-__device__ __forceinline__ f32x4 product(const u32x4& a, const u32x4& b, const f32x4& c) {
-  if constexpr (TYPE == MOE_TYPE_BF16) return mfma16(a, b, c);
-  else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
 // halves of w that are infinite or NaN, as 0xFFFF each
@@ -227,8 +222,11 @@ __global__ void __launch_bounds__(RW == 1 ? 256 : 512, D <= 128 || RW > 1 ? 2 : 
         p[e] = __builtin_amdgcn_exp2f(y[e]);
         if constexpr (EDGE) p[e] = see >> e & 1 ? p[e] : 0.f;
       }
-      l[rt] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
       pf[rt] = u32x4{pack2<TYPE>(p[0], p[1]), pack2<TYPE>(p[2], p[3]), pack2<TYPE>(p[4], p[5]), pack2<TYPE>(p[6], p[7])};
+      // the sum is that of the rounded weights, so that what rounding does to a weight that
+      // outweighs the rest cancels
+#pragma unroll
+      for (int i = 0; i < 4; i++) l[rt] = dot2<TYPE>(pf[rt][i], kOnes<TYPE>, l[rt]);
     }
     const int valid = min(max(total - j0, 0), 8);
 #pragma unroll

@@ -5,7 +5,6 @@
 
 #include <hip/hip_runtime.h>
 
-#include <algorithm>
 #include <cstdint>
 #include <cstdlib>
 

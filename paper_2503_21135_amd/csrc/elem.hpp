@@ -42,7 +42,24 @@ __device__ __forceinline__ float half_hi(uint32_t w) {
   else return fp16_bits_to_f32(w >> 16);
 }
 
-// the same with the type known at run time only
+// a . b + c over two values of a word each, exact products; and two ones
+template <int TYPE>
+__device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float c) {
+  if constexpr (TYPE == MOE_TYPE_BF16)
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, a), __builtin_bit_cast(bf16x2, b), c, false);
+  else
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, a), __builtin_bit_cast(f16x2, b), c, false);
+}
+template <int TYPE> constexpr uint32_t kOnes = TYPE == MOE_TYPE_BF16 ? 0x3F803F80u : 0x3C003C00u;
+
+// 16 x 16 x 32 matrix product of a 16-bit type
+template <int TYPE>
+__device__ __forceinline__ f32x4 product(const u32x4& a, const u32x4& b, const f32x4& c) {
+  if constexpr (TYPE == MOE_TYPE_BF16) return mfma16(a, b, c);
+  else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// reading and rounding with the type known at run time only
 __device__ __forceinline__ float load_elem(const void* p, int64_t i, int type) {
   if (type == MOE_TYPE_FP32) return static_cast<const float*>(p)[i];
   if (type == MOE_TYPE_BF16) return static_cast<float>(static_cast<const __bf16*>(p)[i]);

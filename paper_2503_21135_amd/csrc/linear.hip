@@ -43,22 +43,6 @@ __device__ __forceinline__ uint32_t sixteen() {
   return c;
 }
 
-template <int TYPE>
-__device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float c) {
-  if constexpr (TYPE == MOE_TYPE_BF16)
-    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, a), __builtin_bit_cast(bf16x2, b), c, false);
-  else
-    return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, a), __builtin_bit_cast(f16x2, b), c, false);
-}
-
-template <int TYPE>
-__device__ __forceinline__ f32x4 product(const u32x4& a, const u32x4& b, const f32x4& c) {
-  if constexpr (TYPE == MOE_TYPE_BF16) return mfma16(a, b, c);
-  else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-}
-
-template <int TYPE> constexpr uint32_t kOnes = TYPE == MOE_TYPE_BF16 ? 0x3F803F80u : 0x3C003C00u;
-
 __device__ __forceinline__ void store_y(const LinearArgs& a, int t, int r, float v) {
   if (a.bias) v += a.bias[r];
   store_elem(a.y, t * a.ld_y + r, a.y_type, v);

@@ -2,6 +2,8 @@
 // residual add and the norm before the next block, in one pass over each row:
 //   a = y rsqrt(mean y^2 + eps) w_post,  v = beta r + alpha gate a,
 //   h = v rsqrt(mean v^2 + eps) w_pre.
+#include <algorithm>
+
 #include "elem.hpp"
 
 namespace moe {

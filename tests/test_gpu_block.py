@@ -666,3 +666,16 @@ def test_block_tree_decoding_agrees_with_one_token_at_a_time():
     b, _ = forward(plain, tokens[3:4], 1, None, None)
     assert ((a - b).norm() / b.norm()).item() < 2e-2
     assert all(c.status_value() == 0 for c in caches + plain)
+
+
+def test_example_decodes_with_drafts():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "draft_decode.py")
+    spec = importlib.util.spec_from_file_location("draft_decode", path)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    out, want, steps = mod.main()
+    assert len(out) == len(want) == 60 and 2 <= steps <= 60
+    # the first greedy choices agree; later ones may part where two logits are equal in bf16
+    assert out[:4] == want[:4]
