@@ -538,7 +538,7 @@ int moe_allocate_bits(const double* x, const double* share, int32_t n,
  * order of the sums depends on T, R and K only, so results are bitwise
  * reproducible.  An infinite or NaN activation makes its token's outputs NaN or
  * infinite and no other token's.  Meant for decoding (up to a few hundred
- * tokens); any T gives right results, the weights being read once per 64 tokens.
+ * tokens); the weights are read once per 64 tokens.  T up to 4194240, R up to 2^27.
  */
 int moe_quant_linear(const void* x, int32_t x_type, int64_t ld_x, int32_t T, int32_t K,
                      const uint32_t* codes, int64_t ld_codes,
@@ -564,7 +564,7 @@ int moe_quant_linear(const void* x, int32_t x_type, int64_t ld_x, int32_t T, int
  *   w_post, w_pre   device fp32 [d] or NULL.
  *   r_out   device [T][ld_r_out] of r_type or NULL; may be r itself (same ld).
  *   h       device [T][ld_h] of h_type or NULL; may be r or y itself where type
- *           and ld agree.  r_out and h must not overlap each other.
+ *           and ld agree.  r_out and h overlap neither each other nor any other input.
  * Types are any MOE_TYPE_*; pointers need their type's alignment only.  Norms and
  * sums are fp32; r_out and h are rounded once (h from the unrounded v).  d up to
  * 2^30.  eps >= 0.  Results are bitwise reproducible.
@@ -605,7 +605,8 @@ typedef struct moe_cache {
  * arrays (device int32 [n_seqs + 1], ascending, at most n_tokens), and its pages
  * are table[b*max_pages ...] (device int32 [n_seqs][max_pages], each in [0,
  * n_pages)).  New token i of the sequence lives in slot cache_len[b] + i.
- * max_new is the most new tokens of any sequence, known on the host.  A
+ * max_new is the most new tokens of any sequence, known on the host.  At most
+ * 65535 sequences.  A
  * length, page, position or draft index outside its range is never followed:
  * what it names is skipped, and `status` (device int32 or NULL, never cleared by
  * the library) is set to MOE_ERR_SLOT.
@@ -661,7 +662,8 @@ int moe_tree_attention_plan(const moe_cache_t* C, int32_t n_q_heads, int32_t n_s
  *             sizes (NULL when that is 0); scratch between calls.
  * Scores, softmax and sums are fp32; the softmax weights enter the second
  * product and their own sum rounded to the cache's type, as a matrix operand.  n_q_heads is a multiple of
- * n_heads, at most 64 times it.  Results are bitwise reproducible.
+ * n_heads, at most 64 times it; n_seqs * max_new * n_q_heads at most 2^25.  Results
+ * are bitwise reproducible.
  */
 int moe_tree_attention(const moe_cache_t* C, const int32_t* table, int32_t max_pages,
                        const int32_t* cache_len, int32_t n_seqs, const int32_t* new_off,

@@ -1,5 +1,7 @@
 // cache.hip -- moe_cache_append and moe_cache_keep: the two calls that write the
 // paged key/value cache.
+#include <algorithm>
+
 #include "cache.hpp"
 
 namespace moe {
@@ -289,6 +291,7 @@ extern "C" int moe_cache_append(const moe_cache_t* C, const int32_t* table, int3
   if (n_seqs == 0 || n_tokens == 0 || max_new == 0) return MOE_OK;
   if (int st = check_batch(C, table, max_pages, cache_len, new_off)) return st;
   const int D = C->head_dim;
+  max_new = std::min(max_new, n_tokens);
   if (!k || !v || ld_k < static_cast<int64_t>(C->n_heads) * D || ld_v < static_cast<int64_t>(C->n_heads) * D)
     return MOE_ERR_ARG;
   if (!q != !q_out) return MOE_ERR_ARG;
@@ -317,7 +320,7 @@ extern "C" int moe_cache_keep(const moe_cache_t* C, const int32_t* table, int32_
   using namespace moe;
   using namespace moe::cache;
   if (int st = check_cache(C)) return st;
-  if (n_seqs < 0 || max_keep < 0) return MOE_ERR_ARG;
+  if (n_seqs < 0 || n_seqs > 65535 || max_keep < 0) return MOE_ERR_ARG;
   if (n_seqs == 0) return MOE_OK;
   if (int st = check_batch(C, table, max_pages, cache_len, new_off)) return st;
   if (!n_keep || (max_keep > 0 && !keep) || len_out == cache_len) return MOE_ERR_ARG;

@@ -340,7 +340,7 @@ extern "C" int moe_quant_linear(const void* x, int32_t x_type, int64_t ld_x, int
   using namespace moe;
   if (bits != 4) return MOE_ERR_BITS;
   if (T < 0 || R < 0 || K <= 0 || K > INT32_MAX - 4096 || (group != 64 && group != 128) || K % group) return MOE_ERR_ARG;
-  if (T > 64 * 65535 || R > INT32_MAX - 4096) return MOE_ERR_ARG;
+  if (T > 64 * 65535 || R > (1 << 27)) return MOE_ERR_ARG;   // what one grid holds
   if (!valid_type16(x_type) || (y_type != x_type && y_type != MOE_TYPE_FP32)) return MOE_ERR_ARG;
   if (T == 0 || R == 0) return MOE_OK;
   if (!x || !codes || !sz || !y) return MOE_ERR_ARG;

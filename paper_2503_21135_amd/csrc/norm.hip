@@ -15,6 +15,7 @@ struct NormArgs {
   void *r_out, *h;
   int64_t ld_y, ld_r, gate_row, gate_col, ld_r_out, ld_h;
   float branch, residual, eps;
+  int64_t first;   // the launch's first row
   int T, d, y_type, r_type, gate_type, h_type;
 };
 
@@ -110,7 +111,7 @@ template <int TPR, int NCH>
 __global__ void __launch_bounds__(TPR < kNormThreads ? kNormThreads : TPR) norm_rows_kernel(NormArgs a) {
   constexpr int kRows = TPR < kNormThreads ? kNormThreads / TPR : 1;   // rows of a workgroup
   __shared__ float part[TPR / kWave];
-  const int64_t t = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / TPR;
+  const int64_t t = a.first + static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / TPR;
   if (t >= a.T) return;   // whole waves; never where a row is a workgroup's
   const int tid = threadIdx.x % TPR;
   Raw yr[NCH], rr[NCH];
@@ -198,7 +199,7 @@ __global__ void __launch_bounds__(TPR < kNormThreads ? kNormThreads : TPR) norm_
 // row again for each of the two norms.
 __global__ void __launch_bounds__(kNormThreads) norm_long_kernel(NormArgs a) {
   __shared__ float part[kNormThreads / kWave];
-  const int64_t t = blockIdx.x;
+  const int64_t t = a.first + blockIdx.x;
   float post = a.branch;
   if (a.y && a.w_post) {
     float ss = 0.f;
@@ -237,7 +238,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_long_kernel(NormArgs a) {
 template <int TPR, int NCH>
 void launch_rows(const NormArgs& a, hipStream_t s) {
   constexpr int threads = std::max(TPR, kNormThreads);
-  hipLaunchKernelGGL((norm_rows_kernel<TPR, NCH>), dim3(static_cast<unsigned>(cdiv(a.T, threads / TPR))), dim3(threads), 0, s, a);
+  hipLaunchKernelGGL((norm_rows_kernel<TPR, NCH>), dim3(static_cast<unsigned>(cdiv(a.T - a.first, threads / TPR))), dim3(threads), 0, s, a);
 }
 
 // As many threads as the row has chunks, so that each holds one: more chunks per thread
@@ -250,12 +251,12 @@ void launch_rows(const NormArgs& a, hipStream_t s) {
 void launch_norm(const NormArgs& a, hipStream_t s) {
   const int64_t chunks = cdiv(a.d, kChunk);
   if (chunks <= 64) launch_rows<64, 1>(a, s);
-  else if (chunks <= 128 && a.T >= 1024) launch_rows<64, 2>(a, s);
+  else if (chunks <= 128 && a.T - a.first >= 1024) launch_rows<64, 2>(a, s);
   else if (chunks <= 256) launch_rows<256, 1>(a, s);
   else if (chunks <= 512) launch_rows<512, 1>(a, s);
   else if (chunks <= 1024) launch_rows<1024, 1>(a, s);
   else if (chunks <= 2048) launch_rows<1024, 2>(a, s);
-  else hipLaunchKernelGGL(norm_long_kernel, dim3(static_cast<unsigned>(a.T)), dim3(kNormThreads), 0, s, a);
+  else hipLaunchKernelGGL(norm_long_kernel, dim3(static_cast<unsigned>(a.T - a.first)), dim3(kNormThreads), 0, s, a);
 }
 
 // whether [p, p + n) and [q, q + m) share a byte
@@ -299,8 +300,13 @@ extern "C" int moe_block_norm(const void* y, int32_t y_type, int64_t ld_y, const
     return MOE_ERR_ARG;
   if (r_out && h && overlap(r_out, bytes(ld_r_out, r_type), h, bytes(ld_h, h_type))) return MOE_ERR_ARG;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const NormArgs a{y, r, gate, w_post, w_pre, r_out, h, ld_y, ld_r, gate_row_stride, gate_col_stride,
-                   ld_r_out, ld_h, branch_scale, residual_scale, eps, T, d, y_type, r_type, gate_type, h_type};
-  launch_norm(a, s);
+  NormArgs a{y, r, gate, w_post, w_pre, r_out, h, ld_y, ld_r, gate_row_stride, gate_col_stride,
+             ld_r_out, ld_h, branch_scale, residual_scale, eps, 0, T, d, y_type, r_type, gate_type, h_type};
+  constexpr int64_t kRowsPerLaunch = 1 << 21;   // a grid holds 2^32 threads
+  for (int64_t first = 0; first < T; first += kRowsPerLaunch) {
+    a.first = first;
+    a.T = static_cast<int>(std::min<int64_t>(T, first + kRowsPerLaunch));
+    launch_norm(a, s);
+  }
   return launch_status(s);
 }

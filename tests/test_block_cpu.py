@@ -35,7 +35,7 @@ def test_linear_refusals(lib):
     for b in (2, 3, 8, 16, 5):
         assert call(bits=b) == BITS
     for kw in (dict(group=32), dict(K=200), dict(K=0), dict(T=-1), dict(R=-1), dict(xt=2), dict(xt=5), dict(yt=1),
-               dict(yt=3), dict(x=None), dict(codes=None), dict(sz=None), dict(y=None), dict(ldx=248), dict(ldy=63),
+               dict(yt=3), dict(T=1 << 23), dict(R=1 << 28, ldy=1 << 28), dict(x=None), dict(codes=None), dict(sz=None), dict(y=None), dict(ldx=248), dict(ldy=63),
                dict(ldc=28), dict(srs=0), dict(sgs=-1), dict(K=192, group=128)):
         assert call(**kw) == ARG, kw
     for kw in (dict(x=ODD), dict(ldx=260), dict(codes=ODD), dict(ldc=33), dict(sz=ODD), dict(y=ODD), dict(bias=ODD)):
@@ -100,7 +100,8 @@ def test_attention_refusals(lib):
     for kw in [dict(c=cache_desc(**b)) for b in BAD_CACHE] + [
             dict(c=None), dict(c=cache_desc(v=None)), dict(table=None), dict(pages=0), dict(lens=None), dict(off=None),
             dict(B=-1), dict(N=-1), dict(mx=-1), dict(ml=-1), dict(Hq=3), dict(Hq=0), dict(Hq=130), dict(mw=0),
-            dict(scale=float("inf")), dict(scale=float("nan")), dict(q=None), dict(out=None), dict(ldq=255), dict(ldo=8)]:
+            dict(scale=float("inf")), dict(scale=float("nan")), dict(q=None), dict(out=None), dict(ldq=255), dict(ldo=8),
+            dict(q=OTHER), dict(mx=1 << 24)]:
         assert call(**kw) == ARG, kw
     for kw in (dict(q=ODD), dict(ldq=260), dict(out=OTHER + 1), dict(mask=FAKE + 4), dict(c=cache_desc(k=ODD))):
         assert call(**kw) == ALIGN, kw
@@ -116,7 +117,7 @@ def test_keep_refusals(lib):
     call = caller(lib.moe_cache_keep, dict(c=cache_desc(), table=FAKE, pages=4, lens=FAKE, B=2, off=FAKE, keep=FAKE, mk=4,
                                            n=FAKE, lo=OTHER, st=None, stream=None))
     for kw in [dict(c=cache_desc(**b)) for b in BAD_CACHE] + [
-            dict(table=None), dict(pages=0), dict(lens=None), dict(B=-1), dict(mk=-1), dict(keep=None), dict(n=None),
+            dict(table=None), dict(pages=0), dict(lens=None), dict(B=-1), dict(B=70000), dict(mk=-1), dict(keep=None), dict(n=None),
             dict(lo=FAKE)]:
         assert call(**kw) == ARG, kw
     for kw in (dict(keep=ODD), dict(n=ODD), dict(lo=OTHER + 2)):

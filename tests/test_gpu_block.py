@@ -612,6 +612,45 @@ def test_calls_on_another_stream():
     assert torch.equal(y, other)
 
 
+def test_calls_in_a_captured_graph():
+    """A step captured once and replayed over changing inputs, with eager work in between,
+    gives what the eager calls give each time."""
+    cache, off = batch([900, 2000], [3, 5], 64, 2, 128, BF16, 96)
+    lin = P().QuantLinear(0.02 * torch.randn(512, 256, device="cuda", generator=gen(1)))
+    wo = P().QuantLinear(0.02 * torch.randn(256, 256, device="cuda", generator=gen(2)))
+    x = torch.randn(8, 256, device="cuda", generator=gen(3)).to(BF16)
+    r, w = torch.zeros(8, 256, device="cuda"), torch.ones(256, device="cuda")
+    r_out, h = torch.empty_like(r), torch.empty_like(x)
+    keep = torch.tensor([[0, 2], [1, 4]], dtype=torch.int32, device="cuda")
+    n, lens = torch.tensor([2, 2], dtype=torch.int32, device="cuda"), torch.empty(2, dtype=torch.int32, device="cuda")
+
+    def step():
+        heads = lin(x)
+        q, k, v = (heads[:, 128 * i:128 * (i + 2 - (i > 0))].unflatten(1, (-1, 128)) for i in (0, 2, 3))
+        k, v = k.repeat(1, 2, 1), v.repeat(1, 2, 1)
+        q = cache.append(q, k, v, off, 5)
+        P().moe_block_norm(r, h, y=wo(cache.attend(q, off, 5, 2005).flatten(1)), w_post=w, w_pre=w, r_out=r_out)
+        cache.keep(off, keep, n, len_out=lens)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        x.copy_(torch.randn(8, 256, device="cuda", generator=gen(10 + i)).to(BF16))
+        step()
+        torch.cuda.synchronize()
+        want = [t.clone() for t in (h, r_out, cache.k, cache.v, lens)]
+        h.zero_(), r_out.zero_(), lens.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip((h, r_out, cache.k, cache.v, lens), want):
+            assert torch.equal(a, b)
+
+
 # ------------------------------------------------------------------ the block
 def test_block_tree_decoding_agrees_with_one_token_at_a_time():
     """A tree of drafts through two layers gives, for every path, what the tokens give one
