@@ -232,6 +232,18 @@ def test_norm_in_place_and_bad_rows(d):
         assert torch.equal(r2[i], s["r_out"][i]) and torch.equal(h2[i], s["h"][i])
 
 
+@pytest.mark.parametrize("d", [3, 600])
+def test_norm_of_more_rows_than_a_launch(d):
+    T = (1 << 21) + 5
+    r = torch.randn(T, d, device="cuda", generator=gen(d)).to(BF16)
+    h = torch.empty_like(r)
+    P().moe_block_norm(r, h)
+    for at in (0, (1 << 21) - 3, T - 6):
+        sl = slice(at, at + 6)
+        want = r[sl].double() / (r[sl].double().square().mean(1, keepdim=True) + 1e-6).sqrt()
+        within(h[sl], want, (d / 64 + 72) * E32 * want.abs() + 1.01 * U[BF16] * want.abs())
+
+
 # ------------------------------------------------------------------ the paged cache
 def batch(lens, new, page, Hkv, D, dt, seed, spare=3, fill=None):
     """A cache whose pages are dealt out in random order, and the new tokens' rows."""
