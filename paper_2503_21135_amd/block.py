@@ -83,7 +83,8 @@ class PagedCache:
            (transposed inside the page), bfloat16 or float16
     table  int32 [sequences][max_pages], lens int32 [sequences] (cached tokens)
 
-    The attention's workspace is kept per stream and grows with the calls; calls on
+    The attention's workspace is kept per stream and grows with the calls (it at least
+    doubles, and smaller ones stay, so that captured graphs may use them); calls on
     different streams are independent, except that writers of the same pages must be
     ordered by the caller, as for any device memory.
     """
@@ -105,6 +106,7 @@ class PagedCache:
         self.desc = d
         self._bytes = torch.empty(0, dtype=torch.uint8, device=k.device)
         self._ws: Dict[int, torch.Tensor] = {}
+        self._outgrown = []
         self._need: Dict[tuple, int] = {}
 
     @classmethod
@@ -145,6 +147,9 @@ class PagedCache:
         handle = api._stream(stream, self.k)
         ws = self._ws.get(handle)
         if ws is None or ws.numel() < need:
+            if ws is not None:   # a captured graph may still work in the smaller one
+                self._outgrown.append(ws)
+                need = max(need, 2 * ws.numel())
             ws = self._ws[handle] = _empty((need,), self._bytes, stream)
         return ws
 

@@ -651,6 +651,11 @@ def test_calls_in_a_captured_graph():
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         step()
+    # eager calls that need a larger workspace leave the graph's alone
+    big = torch.randn(8, 64, 128, device="cuda", generator=gen(4)).to(BF16)
+    for s in [torch.cuda.current_stream(), side] + [torch.cuda.Stream() for _ in range(40)]:
+        cache.attend(big, off, 5, 200000, stream=s)
+    torch.cuda.synchronize()
     for i in range(4):
         x.copy_(torch.randn(8, 256, device="cuda", generator=gen(10 + i)).to(BF16))
         step()
