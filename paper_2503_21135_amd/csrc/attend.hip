@@ -246,6 +246,9 @@ __global__ void __launch_bounds__(RW == 1 ? 256 : 512, D <= 128 || RW > 1 ? 2 : 
   };
 
   const int t_full = min(t_end, q.len / kTile);    // tiles before it hold cached tokens alone
+  // this wave's first tile that went through step() as an edge: a wave's n-th alone, or a stage's
+  // first, whose other tiles may lie before t_full
+  const int n_edge = RW == 1 ? max(0, t_full - t_first - wk + KW - 1) / KW : max(0, t_full - t_first) / (KW * KT) * KT;
   if constexpr (RW == 1) {
     // the next tile's keys load behind this one's products; tiles with drafts in them, the
     // last ones, go one at a time
@@ -328,7 +331,7 @@ __global__ void __launch_bounds__(RW == 1 ? 256 : 512, D <= 128 || RW > 1 ? 2 : 
                [&](int v) { return tile.v[16 * v + col][grp ^ (col >> 2)]; }, tile_of(r * KT + j));
       }
     };
-    const int stages = (t_end - t_first + KW * KT - 1) / (KW * KT), full = max(0, t_full - t_first) / (KW * KT);
+    const int stages = (t_end - t_first + KW * KT - 1) / (KW * KT), full = n_edge / KT;
     for (int r = 0; r < full; r++) stage(std::false_type{}, r);
 #pragma unroll 1
     for (int r = full; r < stages; r++) stage(std::true_type{}, r);
@@ -336,12 +339,12 @@ __global__ void __launch_bounds__(RW == 1 ? 256 : 512, D <= 128 || RW > 1 ? 2 : 
   }
 
   if (__any(odd != 0)) {
-    // Infinite and NaN values of drafts were left out of the products, where 0 * NaN would
-    // have reached the rows that do not see them; here they go to the rows that do.
+    // Infinite and NaN values of the edge tiles were left out of the products, where 0 * NaN
+    // would have reached the rows that do not see them; here they go to the rows that do.
 #pragma unroll 1
-    for (int n = 0; n < (t_end - t_first + KW * KT - 1) / (KW * KT) * KT; n++) {
+    for (int n = n_edge; n < (t_end - t_first + KW * KT - 1) / (KW * KT) * KT; n++) {
       const int tf = tile_of(n);
-      if (tf < t_full || tf >= t_end) continue;
+      if (tf >= t_end) continue;
       const int pg = __builtin_amdgcn_readfirstlane(page_of(a.b, s, tf * kTile));
       if (pg < 0) continue;
       const E* kb = static_cast<const E*>(a.kc) + head_at(pg) + (tf * kTile & (P - 1)) * D;
