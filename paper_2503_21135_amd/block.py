@@ -17,7 +17,7 @@ import numpy as np
 import torch
 
 from . import api
-from ._lib import TYPE_BF16, TYPE_FP16, CacheDesc, MoEError
+from ._lib import TYPE_BF16, TYPE_FP16, CacheDesc, MoEError, stream_capturing
 
 _TYPE16 = {torch.bfloat16: TYPE_BF16, torch.float16: TYPE_FP16}
 
@@ -29,6 +29,11 @@ def _empty(shape, like: torch.Tensor, stream) -> torch.Tensor:
         return torch.empty(shape, dtype=like.dtype, device=like.device)
     with torch.cuda.stream(stream):
         return torch.empty(shape, dtype=like.dtype, device=like.device)
+
+
+def _capturing(stream) -> bool:
+    """Whether what is launched on the stream (None: the current one) goes into a graph."""
+    return torch.cuda.is_current_stream_capturing() if stream is None else stream_capturing(stream.cuda_stream)
 
 
 def tree_mask(parents: Sequence[Sequence[int]], device="cuda") -> torch.Tensor:
@@ -84,9 +89,10 @@ class PagedCache:
     table  int32 [sequences][max_pages], lens int32 [sequences] (cached tokens)
 
     The attention's workspace is kept per stream and grows with the calls (it at least
-    doubles, and smaller ones stay, so that captured graphs may use them); calls on
-    different streams are independent, except that writers of the same pages must be
-    ordered by the caller, as for any device memory.
+    doubles).  A call that is being captured works in memory of its graph's own pool
+    instead.  So calls on different streams are independent, and so are replays of
+    graphs that share no pool, except that writers of the same pages must be ordered
+    by the caller, as for any device memory.
     """
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, lens: torch.Tensor,
@@ -106,7 +112,6 @@ class PagedCache:
         self.desc = d
         self._bytes = torch.empty(0, dtype=torch.uint8, device=k.device)
         self._ws: Dict[int, torch.Tensor] = {}
-        self._outgrown = []
         self._need: Dict[tuple, int] = {}
 
     @classmethod
@@ -144,12 +149,12 @@ class PagedCache:
             need = self._need[key] = api.moe_tree_attention_plan(self.desc, *key)[1]
         if need == 0:
             return None
+        if _capturing(stream):   # the stream of a capture is not the one of its replays
+            return _empty((need,), self._bytes, stream)
         handle = api._stream(stream, self.k)
         ws = self._ws.get(handle)
         if ws is None or ws.numel() < need:
-            if ws is not None:   # a captured graph may still work in the smaller one
-                self._outgrown.append(ws)
-                need = max(need, 2 * ws.numel())
+            need = need if ws is None else max(need, 2 * ws.numel())
             ws = self._ws[handle] = _empty((need,), self._bytes, stream)
         return ws
 
