@@ -14,7 +14,7 @@ from typing import Optional, Tuple
 import numpy as np
 import torch
 
-from ._lib import TYPE_BF16, TYPE_FP16, TYPE_FP32, CacheDesc, LayerDesc, MoEError, check, load
+from ._lib import TYPE_BF16, TYPE_FP16, TYPE_FP32, CacheDesc, LayerDesc, MoEError, check, load, stream_capturing
 
 
 def _p(t: Optional[torch.Tensor]):
@@ -187,6 +187,11 @@ def _stream(stream, t: torch.Tensor) -> int:
     """Handle of the stream to work on: the current one of t's device unless given (asked
     for as a number: the Stream object of torch.cuda.current_stream costs 3 us)."""
     return torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else stream.cuda_stream
+
+
+def _capturing(stream) -> bool:
+    """Whether what is launched on the stream (None: the current one) goes into a graph."""
+    return torch.cuda.is_current_stream_capturing() if stream is None else stream_capturing(stream.cuda_stream)
 
 
 def _rows(t: torch.Tensor, T: int, n: int, what: str) -> Tuple[int, int]:

@@ -17,7 +17,7 @@ import numpy as np
 import torch
 
 from . import api
-from ._lib import TYPE_BF16, TYPE_FP16, CacheDesc, MoEError, stream_capturing
+from ._lib import TYPE_BF16, TYPE_FP16, CacheDesc, MoEError
 
 _TYPE16 = {torch.bfloat16: TYPE_BF16, torch.float16: TYPE_FP16}
 
@@ -29,11 +29,6 @@ def _empty(shape, like: torch.Tensor, stream) -> torch.Tensor:
         return torch.empty(shape, dtype=like.dtype, device=like.device)
     with torch.cuda.stream(stream):
         return torch.empty(shape, dtype=like.dtype, device=like.device)
-
-
-def _capturing(stream) -> bool:
-    """Whether what is launched on the stream (None: the current one) goes into a graph."""
-    return torch.cuda.is_current_stream_capturing() if stream is None else stream_capturing(stream.cuda_stream)
 
 
 def tree_mask(parents: Sequence[Sequence[int]], device="cuda") -> torch.Tensor:
@@ -149,7 +144,7 @@ class PagedCache:
             need = self._need[key] = api.moe_tree_attention_plan(self.desc, *key)[1]
         if need == 0:
             return None
-        if _capturing(stream):   # the stream of a capture is not the one of its replays
+        if api._capturing(stream):   # the stream of a capture is not the one of its replays
             return _empty((need,), self._bytes, stream)
         handle = api._stream(stream, self.k)
         ws = self._ws.get(handle)
@@ -220,11 +215,13 @@ class DecoderBlock:
                 next_norm: Optional[torch.Tensor] = None, stream=None) -> None:
         """One layer over the new tokens, in place: r [tokens][d_model] is the residual
         stream, h bf16 of the same shape its norm before this layer (moe_block_norm with
-        norms["attn"]); afterwards h is the norm before the next one (next_norm)."""
+        norms["attn"]); afterwards h is the norm before the next one (next_norm).  Calls on
+        different streams, and replays of different graphs, are independent, each over a
+        cache and tokens of its own."""
         n = self.norms
         a = self.attention(h, cache, new_off, max_new, max_len, positions, mask, stream)
         api.moe_block_norm(r, h, y=a, w_post=n.get("attn_post"), gate=n.get("attn_gate"), w_pre=n["ffn"], r_out=r,
                            eps=self.eps, stream=stream, **self.scales)
-        y = self.moe.forward(h, stream=stream)
+        y = self.moe.forward(h, stream=stream, buffers=self.moe.stream_buffers(h.shape[0], stream))
         api.moe_block_norm(r, h, y=y, w_post=n.get("ffn_post"), gate=n.get("ffn_gate"), w_pre=next_norm, r_out=r,
                            eps=self.eps, stream=stream, **self.scales)

@@ -19,7 +19,7 @@ the switch) and a staging buffer for the host slot list.
 from __future__ import annotations
 
 from dataclasses import dataclass
-from typing import Dict, Optional
+from typing import Dict, Optional, Tuple
 
 import numpy as np
 import torch
@@ -34,7 +34,7 @@ def _u32_to_i32(a: np.ndarray) -> np.ndarray:
 
 @dataclass
 class Buffers:
-    """Per-batch-size device buffers of the pipeline (allocated once)."""
+    """Device buffers of the pipeline for one batch size."""
 
     T: int
     topk_ids: torch.Tensor
@@ -106,6 +106,7 @@ class MoELayer:
         if keep_status and int(self.status.item()) != 0:
             raise MoEError("moe_quant_pack reported status %d" % int(self.status.item()))
         self._bufs: Dict[int, Buffers] = {}
+        self._stream_bufs: Dict[Tuple[int, int], Buffers] = {}
         self.cache16: Dict[int, torch.Tensor] = {}
         # precision of each routed expert's copies per kind: 0 = the 8-bit
         # copies made at load time, b > 0 = requantized at b bits
@@ -206,13 +207,32 @@ class MoELayer:
 
     # ------------------------------------------------------------------ forward
     def buffers(self, T: int) -> Buffers:
-        if T in self._bufs:
-            return self._bufs[T]
+        """The kept set of T tokens: one, whatever the stream, for calls that follow each
+        other.  Calls side by side take sets of their own (new_buffers, stream_buffers)."""
+        if T not in self._bufs:
+            self._bufs[T] = self.new_buffers(T)
+        return self._bufs[T]
+
+    def stream_buffers(self, T: int, stream=None) -> Buffers:
+        """A set of T tokens for calls on one stream (None: the current one); for a call that
+        is being captured, one in its graph's pool."""
+        if api._capturing(stream):
+            return self.new_buffers(T, stream)
+        key = (api._stream(stream, self.router), T)
+        if key not in self._stream_bufs:
+            self._stream_bufs[key] = self.new_buffers(T, stream)
+        return self._stream_bufs[key]
+
+    def new_buffers(self, T: int, stream=None) -> Buffers:
+        """A set of T tokens whose memory is reused in the order of the stream."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.new_buffers(T)
         dev, E, S, k, d = self.device, self.E, self.S, self.k, self.cfg.d_model
         n_split, ffn_bytes = api.moe_ffn_plan(self.desc, T, k)
         rb = api.moe_route_workspace_bytes(T, E, k, S)
         rows = T * (k + S)
-        b = Buffers(
+        return Buffers(
             T=T,
             topk_ids=torch.empty(T, k, dtype=torch.int32, device=dev),
             topk_w=torch.empty(T, k, dtype=torch.float32, device=dev),
@@ -224,11 +244,12 @@ class MoELayer:
             ffn_ws=torch.empty(max(ffn_bytes, 256), dtype=torch.uint8, device=dev),
             y=torch.empty(T, d, dtype=torch.float32, device=dev),
             n_split=n_split)
-        self._bufs[T] = b
-        return b
 
-    def route(self, x: torch.Tensor, bias: Optional[torch.Tensor] = None, stream=None) -> Buffers:
-        b = self.buffers(x.shape[0])
+    def route(self, x: torch.Tensor, bias: Optional[torch.Tensor] = None, stream=None,
+              buffers: Optional[Buffers] = None) -> Buffers:
+        b = self.buffers(x.shape[0]) if buffers is None else buffers
+        if b.T != x.shape[0]:
+            raise MoEError("the buffers are those of %d tokens, x has %d" % (b.T, x.shape[0]))
         api.moe_route_permute(x, self.router, bias, self.k, self.S, b.topk_ids, b.topk_w,
                               b.offsets, b.perm, b.inv, b.route_ws, stream=stream)
         return b
@@ -251,11 +272,12 @@ class MoELayer:
         return b.y
 
     def forward(self, x: torch.Tensor, bias: Optional[torch.Tensor] = None,
-                stream=None) -> torch.Tensor:
-        """x bf16 [T][d_model] on the device -> y fp32 [T][d_model]."""
+                stream=None, buffers: Optional[Buffers] = None) -> torch.Tensor:
+        """x bf16 [T][d_model] on the device -> y fp32 [T][d_model], in `buffers` (the kept set
+        of T tokens unless given)."""
         if x.dtype != torch.bfloat16 or not x.is_cuda or not x.is_contiguous():
             raise MoEError("x must be a contiguous bfloat16 device tensor")
-        b = self.route(x, bias, stream)
+        b = self.route(x, bias, stream, buffers)
         self.ffn(x, b, stream)
         return self.combine(b, stream)
 

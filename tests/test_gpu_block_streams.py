@@ -59,3 +59,125 @@ def test_captured_graphs_of_one_cache_have_their_own_workspace(monkeypatch):
         assert torch.equal(more, want[2])
         for (graph, out), w in zip(graphs, want):
             assert torch.equal(out, w)
+
+
+def small_block(seed=77):
+    import moe_inputs as mi
+    pkg = P()
+    wk = mi.WORKLOADS["tiny"]
+    d, Hq, Hkv, D = wk.layer.d_model, 4, 2, 64
+    g = gen(seed)
+
+    def w(*shape):
+        return 0.05 * torch.randn(*shape, device="cuda", generator=g)
+    return pkg.DecoderBlock(pkg.MoELayer(mi.LayerInputs(wk.layer), device="cuda:0"), w((Hq + 2 * Hkv) * D, d), w(d, Hq * D),
+                            Hq, Hkv, D, dict(attn=1 + w(d), ffn=1 + w(d)), group=64), d
+
+
+class Request:
+    """One batch of tokens with a cache of its own through a block."""
+
+    def __init__(self, block, d, T, seed, ctx=30):
+        self.block, self.T = block, T
+        self.cache = P().PagedCache.create(1, 256, block.Hkv, block.D, page_size=32)
+        self.cache.k.copy_(torch.randn(self.cache.k.shape, device="cuda", generator=gen(seed)))
+        self.cache.v.copy_(torch.randn(self.cache.v.shape, device="cuda", generator=gen(seed + 1)))
+        self.cache.lens.fill_(ctx)
+        self.ctx = ctx
+        self.off = torch.tensor([0, T], dtype=torch.int32, device="cuda")
+        self.r0 = torch.randn(T, d, device="cuda", generator=gen(seed + 2))
+        self.r, self.h = self.r0.clone(), torch.empty(T, d, dtype=BF16, device="cuda")
+        self.reset()
+
+    def reset(self):
+        self.r.copy_(self.r0)
+        P().moe_block_norm(self.r, self.h, w_pre=self.block.norms["attn"])
+
+    def step(self, stream=None):
+        self.block.forward(self.r, self.h, self.cache, self.off, self.T, self.ctx + self.T, stream=stream)
+
+    def result(self):
+        return self.r.clone(), self.h.clone()
+
+
+def note_ffn_memory(monkeypatch):
+    """Byte ranges that each call of the expert FFN writes."""
+    from paper_2503_21135_amd import api
+    seen = []
+    call = api.moe_expert_ffn_mixed
+
+    def noted(desc, x, k, offsets, perm, o, ws, **kw):
+        seen.append([(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in (offsets, perm, o, ws)])
+        return call(desc, x, k, offsets, perm, o, ws, **kw)
+    monkeypatch.setattr(api, "moe_expert_ffn_mixed", noted)
+    return seen
+
+
+def disjoint(calls):
+    ranges = [r for c in calls for r in c]
+    return all(b <= c or d <= a for i, (a, b) in enumerate(ranges) for c, d in ranges[:i])
+
+
+def test_block_on_two_streams(monkeypatch):
+    """Two batches of equal size through one block on two streams give what they give alone."""
+    block, d = small_block()
+    reqs = [Request(block, d, 24, 100 + 10 * i) for i in range(2)]
+    want = []
+    for q in reqs:
+        q.step()
+        want.append(q.result())
+        q.reset()
+    torch.cuda.synchronize()
+    seen = note_ffn_memory(monkeypatch)
+    streams = [torch.cuda.Stream() for _ in reqs]
+    for q, s in zip(reqs, streams):      # one after the other
+        q.step(s)
+        torch.cuda.synchronize()
+    assert len(seen) == 2 and disjoint(seen), "calls on two streams share the expert layer's buffers"
+    for _ in range(20):
+        for q in reqs:
+            q.reset()
+        torch.cuda.synchronize()
+        for q, s in zip(reqs, streams):
+            q.step(s)
+        torch.cuda.synchronize()
+        for q, w in zip(reqs, want):
+            assert all(torch.equal(a, b) for a, b in zip(q.result(), w))
+    # and with each stream made the current one
+    for q, s in zip(reqs, streams):
+        q.reset()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            q.step()
+        torch.cuda.synchronize()
+    assert seen[-2:] == seen[:2]
+    assert all(torch.equal(a, b) for q, w in zip(reqs, want) for a, b in zip(q.result(), w))
+
+
+def test_block_in_two_captured_graphs(monkeypatch):
+    """The same as two graphs that are replayed side by side, with eager calls next to them."""
+    block, d = small_block(78)
+    reqs = [Request(block, d, 24, 200 + 10 * i) for i in range(3)]
+    want = []
+    for q in reqs:
+        q.step()
+        want.append(q.result())
+        q.reset()
+    torch.cuda.synchronize()
+    seen = note_ffn_memory(monkeypatch)
+    graphs = [capture(q.step)[0] for q in reqs[:2]]
+    reqs[2].step()
+    torch.cuda.synchronize()
+    assert len(seen) == 3 and disjoint(seen), "calls that may run side by side share the expert layer's buffers"
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for _ in range(10):
+        for q in reqs:
+            q.reset()
+        torch.cuda.synchronize()
+        for graph, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                graph.replay()
+        reqs[2].step()
+        torch.cuda.synchronize()
+        for q, w in zip(reqs, want):
+            assert all(torch.equal(a, b) for a, b in zip(q.result(), w))
