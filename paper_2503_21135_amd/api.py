@@ -194,6 +194,14 @@ def _capturing(stream) -> bool:
     return torch.cuda.is_current_stream_capturing() if stream is None else stream_capturing(stream.cuda_stream)
 
 
+def _empty(shape, dtype: torch.dtype, device, stream) -> torch.Tensor:
+    """A new tensor whose memory is reused in the order of the stream that works on it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _rows(t: torch.Tensor, T: int, n: int, what: str) -> Tuple[int, int]:
     """(data pointer, row stride) of a [T][n] device tensor whose rows are contiguous."""
     if t.shape == (T, n) and t.is_cuda:

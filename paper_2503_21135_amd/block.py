@@ -22,15 +22,6 @@ from ._lib import TYPE_BF16, TYPE_FP16, CacheDesc, MoEError
 _TYPE16 = {torch.bfloat16: TYPE_BF16, torch.float16: TYPE_FP16}
 
 
-def _empty(shape, like: torch.Tensor, stream) -> torch.Tensor:
-    """A new tensor of the type of `like` whose memory is reused in the order of the
-    stream that works on it."""
-    if stream is None:
-        return torch.empty(shape, dtype=like.dtype, device=like.device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=like.dtype, device=like.device)
-
-
 def tree_mask(parents: Sequence[Sequence[int]], device="cuda") -> torch.Tensor:
     """Mask words int64 [tokens][ceil(most drafts / 64)] of drafted trees: parents[b][i] is
     the index, below i, of the draft that draft i of sequence b continues, -1 for one that
@@ -71,7 +62,7 @@ class QuantLinear:
     def __call__(self, x: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """x [T][K] bf16 or fp16 -> [T][R] (a new tensor of x's type unless `out` is given)."""
         if out is None:
-            out = _empty((x.shape[0], self.R), x, stream)
+            out = api._empty((x.shape[0], self.R), x.dtype, x.device, stream)
         api.moe_quant_linear(x, self.codes, self.sz, out, bias=self.bias, stream=stream)
         return out
 
@@ -105,7 +96,6 @@ class PagedCache:
         d.k, d.v = k.data_ptr(), v.data_ptr()
         d.n_pages, d.n_heads, d.page_size, d.head_dim, d.type = n_pages, heads, page, D, _TYPE16[k.dtype]
         self.desc = d
-        self._bytes = torch.empty(0, dtype=torch.uint8, device=k.device)
         self._ws: Dict[int, torch.Tensor] = {}
         self._need: Dict[tuple, int] = {}
 
@@ -130,7 +120,7 @@ class PagedCache:
                q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
         """Rotate q and k, store k and v of the new tokens; returns the rotated q."""
         if q is not None and q_out is None:
-            q_out = _empty(q.shape, q, stream)
+            q_out = api._empty(q.shape, q.dtype, q.device, stream)
         api.moe_cache_append(self.desc, self.table, self.lens, new_off, max_new, q, k, v, q_out, positions, cos,
                              sin, interleaved, self.status, stream)
         return q_out
@@ -145,12 +135,12 @@ class PagedCache:
         if need == 0:
             return None
         if api._capturing(stream):   # the stream of a capture is not the one of its replays
-            return _empty((need,), self._bytes, stream)
+            return api._empty((need,), torch.uint8, self.k.device, stream)
         handle = api._stream(stream, self.k)
         ws = self._ws.get(handle)
         if ws is None or ws.numel() < need:
             need = need if ws is None else max(need, 2 * ws.numel())
-            ws = self._ws[handle] = _empty((need,), self._bytes, stream)
+            ws = self._ws[handle] = api._empty((need,), torch.uint8, self.k.device, stream)
         return ws
 
     def attend(self, q: torch.Tensor, new_off: torch.Tensor, max_new: int, max_len: int,
@@ -160,7 +150,7 @@ class PagedCache:
         cached plus new tokens of a sequence as far as the host knows it (sets how the work is
         split).  scale: head_dim ** -0.5 unless given."""
         if out is None:
-            out = _empty(q.shape, q, stream)
+            out = api._empty(q.shape, q.dtype, q.device, stream)
         api.moe_tree_attention(self.desc, self.table, self.lens, new_off, max_new, max_len, q, out,
                                q.shape[2] ** -0.5 if scale is None else scale, mask,
                                self._workspace(q.shape[1], max_new, max_len, stream), self.status, stream)
@@ -172,7 +162,7 @@ class PagedCache:
         lengths.  `lens` itself changes only when the caller copies them there, after the
         last layer's cache has been kept."""
         if len_out is None:
-            len_out = _empty(self.lens.shape, self.lens, stream)
+            len_out = api._empty(self.lens.shape, self.lens.dtype, self.lens.device, stream)
         api.moe_cache_keep(self.desc, self.table, self.lens, new_off, keep, n_keep, len_out, self.status, stream)
         return len_out
 

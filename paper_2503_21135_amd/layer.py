@@ -18,6 +18,7 @@ the switch) and a staging buffer for the host slot list.
 """
 from __future__ import annotations
 
+import math
 from dataclasses import dataclass
 from typing import Dict, Optional, Tuple
 
@@ -106,7 +107,8 @@ class MoELayer:
         if keep_status and int(self.status.item()) != 0:
             raise MoEError("moe_quant_pack reported status %d" % int(self.status.item()))
         self._bufs: Dict[int, Buffers] = {}
-        self._stream_bufs: Dict[Tuple[int, int], Buffers] = {}
+        # per stream: the allocation, and the sets of each batch size that lie in it
+        self._stream_bufs: Dict[int, Tuple[torch.Tensor, Dict[int, Buffers]]] = {}
         self.cache16: Dict[int, torch.Tensor] = {}
         # precision of each routed expert's copies per kind: 0 = the 8-bit
         # copies made at load time, b > 0 = requantized at b bits
@@ -214,36 +216,48 @@ class MoELayer:
         return self._bufs[T]
 
     def stream_buffers(self, T: int, stream=None) -> Buffers:
-        """A set of T tokens for calls on one stream (None: the current one); for a call that
-        is being captured, one in its graph's pool."""
+        """A set of T tokens for calls on one stream (None: the current one), valid until the
+        next set of that stream: all of them lie in one allocation per stream, which at least
+        doubles when it grows.  For a call that is being captured, a set in its graph's pool."""
         if api._capturing(stream):
             return self.new_buffers(T, stream)
-        key = (api._stream(stream, self.router), T)
-        if key not in self._stream_bufs:
-            self._stream_bufs[key] = self.new_buffers(T, stream)
-        return self._stream_bufs[key]
+        handle = api._stream(stream, self.router)
+        room, sets = self._stream_bufs.get(handle, (None, {}))
+        b = sets.get(T)
+        if b is None:
+            n_split, fields = self._fields(T)
+            starts, end = [], 0
+            for shape, dtype in fields.values():
+                starts.append(end)
+                end += (math.prod(shape) * dtype.itemsize + 255) // 256 * 256
+            if room is None or room.numel() < end or len(sets) >= 4096:
+                if room is None or room.numel() < end:
+                    end = end if room is None else max(end, 2 * room.numel())
+                    room = api._empty((end,), torch.uint8, self.device, stream)
+                self._stream_bufs[handle] = room, (sets := {})
+            b = sets[T] = Buffers(T=T, n_split=n_split, **{
+                name: room[at:at + math.prod(shape) * dtype.itemsize].view(dtype).view(shape)
+                for at, (name, (shape, dtype)) in zip(starts, fields.items())})
+        return b
 
     def new_buffers(self, T: int, stream=None) -> Buffers:
         """A set of T tokens whose memory is reused in the order of the stream."""
-        if stream is not None:
-            with torch.cuda.stream(stream):
-                return self.new_buffers(T)
-        dev, E, S, k, d = self.device, self.E, self.S, self.k, self.cfg.d_model
+        n_split, fields = self._fields(T)
+        return Buffers(T=T, n_split=n_split, **{name: api._empty(shape, dtype, self.device, stream)
+                                                for name, (shape, dtype) in fields.items()})
+
+    def _fields(self, T: int):
+        """(n_split, shape and type of each of the tensors) of a set of T tokens."""
+        E, S, k, d = self.E, self.S, self.k, self.cfg.d_model
         n_split, ffn_bytes = api.moe_ffn_plan(self.desc, T, k)
         rb = api.moe_route_workspace_bytes(T, E, k, S)
         rows = T * (k + S)
-        return Buffers(
-            T=T,
-            topk_ids=torch.empty(T, k, dtype=torch.int32, device=dev),
-            topk_w=torch.empty(T, k, dtype=torch.float32, device=dev),
-            offsets=torch.empty(E + S + 1, dtype=torch.int32, device=dev),
-            perm=torch.empty(max(rows, 1), dtype=torch.int32, device=dev),
-            inv=torch.empty(T, k + S, dtype=torch.int32, device=dev),
-            route_ws=torch.empty(max(rb, 256), dtype=torch.uint8, device=dev),
-            o=torch.empty(n_split, max(rows, 1), d, dtype=torch.float32, device=dev),
-            ffn_ws=torch.empty(max(ffn_bytes, 256), dtype=torch.uint8, device=dev),
-            y=torch.empty(T, d, dtype=torch.float32, device=dev),
-            n_split=n_split)
+        return n_split, dict(
+            topk_ids=((T, k), torch.int32), topk_w=((T, k), torch.float32),
+            offsets=((E + S + 1,), torch.int32), perm=((max(rows, 1),), torch.int32),
+            inv=((T, k + S), torch.int32), route_ws=((max(rb, 256),), torch.uint8),
+            o=((n_split, max(rows, 1), d), torch.float32), ffn_ws=((max(ffn_bytes, 256),), torch.uint8),
+            y=((T, d), torch.float32))
 
     def route(self, x: torch.Tensor, bias: Optional[torch.Tensor] = None, stream=None,
               buffers: Optional[Buffers] = None) -> Buffers:

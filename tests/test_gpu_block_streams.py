@@ -181,3 +181,34 @@ def test_block_in_two_captured_graphs(monkeypatch):
         torch.cuda.synchronize()
         for q, w in zip(reqs, want):
             assert all(torch.equal(a, b) for a, b in zip(q.result(), w))
+
+
+def test_block_memory_stays_bounded_over_many_sizes():
+    """Batches of ever other sizes through a block hold memory for the largest few times over,
+    not for each size, and give what they give with buffers of their own."""
+    block, d = small_block(79)
+    torch.cuda.synchronize()
+    sizes = list(range(1, 160))
+    req = Request(block, d, 160, 300)
+
+    def one(T):
+        q = Request.__new__(Request)
+        q.block, q.T, q.cache, q.ctx = block, T, req.cache, req.ctx
+        q.off = torch.tensor([0, T], dtype=torch.int32, device="cuda")
+        q.r, q.h = req.r0[:T].clone(), torch.empty(T, d, dtype=BF16, device="cuda")
+        P().moe_block_norm(q.r, q.h, w_pre=block.norms["attn"])
+        q.step()
+        return q.r, q.h
+    one(1)
+    own = block.moe.new_buffers(160)
+    largest = sum(t.numel() * t.element_size() for t in vars(own).values() if torch.is_tensor(t))
+    del own
+    before = torch.cuda.memory_allocated()
+    first = {T: one(T) for T in (3, 40, 41)}
+    for T in sizes + sizes[::-1]:
+        one(T)
+    again = {T: one(T) for T in first}
+    assert all(torch.equal(a, b) for T in first for a, b in zip(first[T], again[T]))
+    del first, again
+    held = torch.cuda.memory_allocated() - before
+    assert held <= 4 * largest, "%d bytes held, a batch of the largest size needs %d" % (held, largest)
