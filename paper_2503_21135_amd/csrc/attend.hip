@@ -167,9 +167,10 @@ __global__ void __launch_bounds__(RW == 1 ? 256 : 512, D <= 128 || RW > 1 ? 2 : 
     for (int v = 0; v < NV; v++) vf[v] = *reinterpret_cast<const u32x4*>(p + 16 * v * P + v_off);
   };
 
+  const int t_full = min(t_end, q.len / kTile);    // tiles before it hold cached tokens alone
   uint32_t odd = 0;   // not 0: this wave left values out that are not finite
   // One tile: scores, softmax state, and the second product.  EDGE: slots that not
-  // everybody sees are among the tile's (drafts, or none at all).
+  // everybody sees (drafts, or none at all) may be among the tile's, and are from t_full on.
   // get_k and get_v give the tile's operands, from registers or LDS.
   auto step = [&](auto edge_c, auto get_k, auto get_v, int t) {
     constexpr bool EDGE = decltype(edge_c)::value;
@@ -229,14 +230,15 @@ __global__ void __launch_bounds__(RW == 1 ? 256 : 512, D <= 128 || RW > 1 ? 2 : 
       for (int i = 0; i < 4; i++) l[rt] = dot2<TYPE>(pf[rt][i], kOnes<TYPE>, l[rt]);
     }
     const int valid = min(max(total - j0, 0), 8);
+    const uint32_t scrub = RW > 1 && t < t_full ? 0u : 0xFFFFFFFFu;   // a stage's edge may be behind this tile of it
 #pragma unroll
     for (int v = 0; v < NV; v++) {
       u32x4 w = get_v(v);
       if constexpr (EDGE)
 #pragma unroll
-        for (int i = 0; i < 4; i++) {   // slots past the last token, and what is not finite, as zeros
+        for (int i = 0; i < 4; i++) {   // slots past the last token, and what is not finite but not seen by all, as zeros
           const uint32_t in = valid >= 2 * i + 2 ? 0xFFFFFFFFu : (valid == 2 * i + 1 ? 0xFFFFu : 0u);
-          const uint32_t bad = not_finite<TYPE>(w[i]) & in;
+          const uint32_t bad = not_finite<TYPE>(w[i]) & in & scrub;
           w[i] &= in & ~bad;
           odd |= bad;
         }
@@ -245,10 +247,6 @@ __global__ void __launch_bounds__(RW == 1 ? 256 : 512, D <= 128 || RW > 1 ? 2 : 
     }
   };
 
-  const int t_full = min(t_end, q.len / kTile);    // tiles before it hold cached tokens alone
-  // this wave's first tile that went through step() as an edge: a wave's n-th alone, or a stage's
-  // first, whose other tiles may lie before t_full
-  const int n_edge = RW == 1 ? max(0, t_full - t_first - wk + KW - 1) / KW : max(0, t_full - t_first) / (KW * KT) * KT;
   if constexpr (RW == 1) {
     // the next tile's keys load behind this one's products; tiles with drafts in them, the
     // last ones, go one at a time
@@ -331,7 +329,7 @@ __global__ void __launch_bounds__(RW == 1 ? 256 : 512, D <= 128 || RW > 1 ? 2 : 
                [&](int v) { return tile.v[16 * v + col][grp ^ (col >> 2)]; }, tile_of(r * KT + j));
       }
     };
-    const int stages = (t_end - t_first + KW * KT - 1) / (KW * KT), full = n_edge / KT;
+    const int stages = (t_end - t_first + KW * KT - 1) / (KW * KT), full = max(0, t_full - t_first) / (KW * KT);
     for (int r = 0; r < full; r++) stage(std::false_type{}, r);
 #pragma unroll 1
     for (int r = full; r < stages; r++) stage(std::true_type{}, r);
@@ -339,12 +337,12 @@ __global__ void __launch_bounds__(RW == 1 ? 256 : 512, D <= 128 || RW > 1 ? 2 : 
   }
 
   if (__any(odd != 0)) {
-    // Infinite and NaN values of the edge tiles were left out of the products, where 0 * NaN
+    // Infinite and NaN values of tiles from t_full on were left out of the products, where 0 * NaN
     // would have reached the rows that do not see them; here they go to the rows that do.
 #pragma unroll 1
-    for (int n = n_edge; n < (t_end - t_first + KW * KT - 1) / (KW * KT) * KT; n++) {
+    for (int n = 0; n < (t_end - t_first + KW * KT - 1) / (KW * KT) * KT; n++) {
       const int tf = tile_of(n);
-      if (tf >= t_end) continue;
+      if (tf < t_full || tf >= t_end) continue;
       const int pg = __builtin_amdgcn_readfirstlane(page_of(a.b, s, tf * kTile));
       if (pg < 0) continue;
       const E* kb = static_cast<const E*>(a.kc) + head_at(pg) + (tf * kTile & (P - 1)) * D;
