@@ -660,10 +660,11 @@ int moe_tree_attention_plan(const moe_cache_t* C, int32_t n_q_heads, int32_t n_s
  *             rows of q 16-byte aligned.  out must not overlap q or the cache.
  *   ws        device workspace of moe_tree_attention_plan's bytes for the same
  *             sizes (NULL when that is 0); scratch between calls.
- * Scores, softmax and sums are fp32; the softmax weights enter the second
- * product and their own sum rounded to the cache's type, as a matrix operand.  n_q_heads is a multiple of
- * n_heads, at most 64 times it; n_seqs * max_new * n_q_heads at most 2^25.  Results
- * are bitwise reproducible.
+ * Scores, softmax and sums are fp32; the softmax weights enter the second product
+ * and their own sum rounded to the cache's type, as a matrix operand (in fp16 a
+ * weight below 2^-32 of the row's largest may count as zero).  n_q_heads is a
+ * multiple of n_heads, at most 64 times it; n_seqs * max_new * n_q_heads at most
+ * 2^25.  Results are bitwise reproducible.
  */
 int moe_tree_attention(const moe_cache_t* C, const int32_t* table, int32_t max_pages,
                        const int32_t* cache_len, int32_t n_seqs, const int32_t* new_off,

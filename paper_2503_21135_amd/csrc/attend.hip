@@ -20,7 +20,12 @@ namespace cache {
 namespace {
 
 constexpr int kTile = 32;        // keys of a step; divides every page size
-constexpr float kSlack = 8.f;    // weights stay below 2^8: finite in fp16, and exact enough in both types
+// A row's weights are 2^(score - maximum + kLift), with a maximum that may lag 2^kSlack behind.
+// In fp16 the lift of 7 keeps the largest finite (2^15) and gives weights that are small beside it
+// their place: normal down to 2^-21 of the maximum, zero only below 2^-32 (unlifted, a million
+// keys of 2^-26 each, 1.6 % of the sum, counted for nothing).  bf16 has fp32's range.
+constexpr float kSlack = 8.f;
+template <int TYPE> constexpr float kLift = TYPE == MOE_TYPE_FP16 ? 7.f : 0.f;
 constexpr int kMaxSplit = 64;    // the joining wave holds one part's statistics per lane
 
 struct AttendArgs {
@@ -132,7 +137,7 @@ __global__ void __launch_bounds__(RW == 1 ? 256 : 512, D <= 128 || RW > 1 ? 2 : 
     for (int c = 0; c < NC; c++) qf[rt][c] = *reinterpret_cast<const u32x4*>(p + 32 * c) ^ u32x4{a.flip, a.flip, a.flip, a.flip};
   }
   f32x4 o[RT][NV];
-  float m[RT], ms[RT], l[RT];   // maximum, the same scaled, sum
+  float m[RT], ms[RT], l[RT];   // maximum, the same scaled less the lift, sum
 #pragma unroll
   for (int rt = 0; rt < RT; rt++) {
     m[rt] = ms[rt] = -INFINITY;
@@ -200,12 +205,12 @@ __global__ void __launch_bounds__(RW == 1 ? 256 : 512, D <= 128 || RW > 1 ? 2 : 
         return fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
       };
       // A row's maximum moves only when a score passes it by kSlack: until then weights
-      // stay below 2^kSlack, and no lane asks the others for theirs.  (A row that has seen
+      // stay below 2^(kSlack + kLift), and no lane asks the others for theirs.  (A row that has seen
       // nothing has -infinity, which any score passes.)
-      if (__any(!(most(y) <= kSlack))) {
-        const bool moves = !(rows_max(most(y)) <= kSlack);    // this row, whatever its neighbours do
+      if (__any(!(most(y) <= kSlack + kLift<TYPE>))) {
+        const bool moves = !(rows_max(most(y)) <= kSlack + kLift<TYPE>);    // this row, whatever its neighbours do
         const float m2 = moves ? fmaxf(m[rt], rows_max(most(x))) : m[rt];
-        const float ms2 = m2 == -INFINITY ? 0.f : m2 * a.scale2;
+        const float ms2 = m2 == -INFINITY ? 0.f : m2 * a.scale2 - kLift<TYPE>;
         const float f = m[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms[rt] - ms2);
         l[rt] *= f;
 #pragma unroll
@@ -365,7 +370,7 @@ __global__ void __launch_bounds__(RW == 1 ? 256 : 512, D <= 128 || RW > 1 ? 2 : 
           }
           x = rows_sum(x);
           const bool sees = seen8(a, q.off + tok[rt], tok[rt], q.n, tf * kTile + key - q.len) & 1;
-          const float p = __builtin_amdgcn_exp2f(__fmaf_rn(x, a.scale2, m[rt] == -INFINITY ? 0.f : -(m[rt] * a.scale2)));
+          const float p = __builtin_amdgcn_exp2f(__fmaf_rn(x, a.scale2, m[rt] == -INFINITY ? 0.f : -ms[rt]));
 #pragma unroll
           for (int v = 0; v < NV; v++)
 #pragma unroll

@@ -1,11 +1,12 @@
-"""moe_tree_attention with values that are not finite among the cached tokens, on every way
+"""moe_tree_attention where values or weights are extreme: values that are not finite among the
+cached tokens, and weights that are far below the largest, on every way
 that rows and keys are laid over waves (rows per key head and head size choose it)."""
 import math
 
 import pytest
 import torch
 
-from test_gpu_block import BF16, FP16, batch, gen
+from test_gpu_block import BF16, FP16, P, batch, gen, within
 
 pytestmark = pytest.mark.gpu
 
@@ -33,3 +34,30 @@ def test_cached_values_that_are_not_finite_reach_every_row(D, new, Hq, dt):
             cache.v[at] = was
             assert not torch.isfinite(out[:, :, 2]).any(), "value %s in tile %d was lost" % (val, tile)
             assert torch.equal(out[:, :, rest], clean[:, :, rest]), tile
+
+
+@pytest.mark.parametrize("D,new", [(64, 1), (64, 30), (64, 40), (128, 1), (128, 20), (128, 70), (256, 3), (256, 40)])
+def test_many_small_weights_count(D, new):
+    """2^20 fp16 keys of 2^-26.5 of the largest weight each, beside 8 of the largest (one in each
+    of the first tiles, so that every wave has seen it).  A weight below fp16's normal range
+    is off by up to 2^-25 where the largest is stored as 2^7, so the sum by up to N 2^-32 of the
+    largest; the fp32 sum of weights by up to 2^-11 of itself (8192 steps of half a unit in the
+    last place of 2^7)."""
+    N, page, tops = 1 << 20, 1024, 8
+    k = torch.zeros(N // page + 1, 1, page, D, dtype=FP16, device="cuda")
+    v = torch.ones(N // page + 1, 1, D, page, dtype=FP16, device="cuda")
+    at = 32 * torch.arange(tops, device="cuda")
+    k[0, 0, at, 0] = 16
+    v[0, 0, :, at] = 0
+    k[N // page, 0, :new, 0] = -1000       # the new tokens' own keys weigh nothing
+    table = torch.arange(N // page + 1, dtype=torch.int32, device="cuda")[None]
+    cache = P().PagedCache(k, v, table, torch.tensor([N], dtype=torch.int32, device="cuda"))
+    q = torch.zeros(new, 1, D, dtype=FP16, device="cuda")
+    q[:, 0, 0] = 1.0
+    off = torch.tensor([0, new], dtype=torch.int32, device="cuda")
+    small = (N - tops) * 2.0 ** -26.5
+    want = torch.full((new, 1, D), small / (tops + small), dtype=torch.float64, device="cuda")
+    bound = N * 2.0 ** -32 / tops + (2 * 2.0 ** -11 + 2.0 ** -14) * want
+    for guess in (0, N + new):             # the keys in one part, and in many
+        out = cache.attend(q, off, new, guess, scale=26.5 * math.log(2) / 16)
+        within(out, want, bound, "small weights")
