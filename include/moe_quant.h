@@ -562,9 +562,10 @@ int moe_quant_linear(const void* x, int32_t x_type, int64_t ld_x, int32_t T, int
  *           c*gate_col_stride, gate_col_stride 0 or 1 (per channel: strides 0, 1;
  *           per token: s, 0; per element: s, 1).
  *   w_post, w_pre   device fp32 [d] or NULL.
- *   r_out   device [T][ld_r_out] of r_type or NULL; may be r itself (same ld).
- *   h       device [T][ld_h] of h_type or NULL; may be r or y itself where type
- *           and ld agree.  r_out and h overlap neither each other nor any other input.
+ *   r_out   device [T][ld_r_out] of r_type or NULL.
+ *   h       device [T][ld_h] of h_type or NULL.
+ *           Either may be r, y or a gate per element itself, where type and ld agree.
+ *           They overlap neither each other nor any input in another way (MOE_ERR_ARG).
  * Types are any MOE_TYPE_*; pointers need their type's alignment only.  Norms and
  * sums are fp32; r_out and h are rounded once (h from the unrounded v).  d up to
  * 2^30.  eps >= 0.  Results are bitwise reproducible.

@@ -257,7 +257,8 @@ def moe_block_norm(r: torch.Tensor, h: Optional[torch.Tensor] = None, y: Optiona
     v = residual_scale r + branch_scale gate rms(y) w_post;  r_out = v;  h = rms(v) w_pre.
 
     gate is [d] (per channel), [T][1] (per token) or [T][d]; without y, v is the scaled
-    residual alone; without w_post, y is taken as it is.  r_out may be r, h may be r or y.
+    residual alone; without w_post, y is taken as it is.  r_out and h may each be r, y or a
+    gate per element, in place.
     """
     T, d = r.shape
     g, g_type, g_row, g_col = None, 0, 0, 0

@@ -18,6 +18,12 @@ inline bool aligned_to(const void* p, int bytes) {
   return (reinterpret_cast<uintptr_t>(p) & static_cast<uintptr_t>(bytes - 1)) == 0;
 }
 
+// whether [p, p + n) and [q, q + m) share a byte
+inline bool overlap(const void* p, int64_t n, const void* q, int64_t m) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return p && q && a < b + static_cast<uintptr_t>(m) && b < a + static_cast<uintptr_t>(n);
+}
+
 template <int TYPE> struct ElemOf;
 template <> struct ElemOf<MOE_TYPE_BF16> { typedef __bf16 type; };
 template <> struct ElemOf<MOE_TYPE_FP16> { typedef _Float16 type; };

@@ -259,12 +259,6 @@ void launch_norm(const NormArgs& a, hipStream_t s) {
   else hipLaunchKernelGGL(norm_long_kernel, dim3(static_cast<unsigned>(a.T - a.first)), dim3(kNormThreads), 0, s, a);
 }
 
-// whether [p, p + n) and [q, q + m) share a byte
-bool overlap(const void* p, int64_t n, const void* q, int64_t m) {
-  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-  return p && q && a < b + static_cast<uintptr_t>(m) && b < a + static_cast<uintptr_t>(n);
-}
-
 }  // namespace
 }  // namespace moe
 
@@ -295,9 +289,14 @@ extern "C" int moe_block_norm(const void* y, int32_t y_type, int64_t ld_y, const
     if (!in || !out || !overlap(in, bytes(ld_in, type_in), out, bytes(ld_out, type_out))) return false;
     return in != out || type_in != type_out || (T > 1 && ld_in != ld_out);
   };
-  if (clash(r, ld_r, r_type, r_out, ld_r_out, r_type) || clash(r, ld_r, r_type, h, ld_h, h_type) ||
-      (y && (clash(y, ld_y, y_type, r_out, ld_r_out, r_type) || clash(y, ld_y, y_type, h, ld_h, h_type))))
-    return MOE_ERR_ARG;
+  const auto spoils = [&](const void* out, int64_t ld, int type) {   // an output that lies over an input
+    if (clash(r, ld_r, r_type, out, ld, type) || (y && clash(y, ld_y, y_type, out, ld, type))) return true;
+    if (gate && gate_col_stride ? clash(gate, gate_row_stride, gate_type, out, ld, type)
+                                : overlap(gate, ((T - 1) * gate_row_stride + 1) * type_bytes(gate_type), out, bytes(ld, type)))
+      return true;
+    return overlap(w_post, 4 * static_cast<int64_t>(d), out, bytes(ld, type)) || overlap(w_pre, 4 * static_cast<int64_t>(d), out, bytes(ld, type));
+  };
+  if (spoils(r_out, ld_r_out, r_type) || spoils(h, ld_h, h_type)) return MOE_ERR_ARG;
   if (r_out && h && overlap(r_out, bytes(ld_r_out, r_type), h, bytes(ld_h, h_type))) return MOE_ERR_ARG;
   hipStream_t s = static_cast<hipStream_t>(stream);
   NormArgs a{y, r, gate, w_post, w_pre, r_out, h, ld_y, ld_r, gate_row_stride, gate_col_stride,
