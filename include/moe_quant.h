@@ -658,7 +658,8 @@ int moe_tree_attention_plan(const moe_cache_t* C, int32_t n_q_heads, int32_t n_s
  * key/value head h / (n_q_heads / n_heads).  A token that sees nothing gets zeros.
  * What a token does not see has no effect on it, NaN and infinities included.
  *   q, out    device [n_tokens][ld] of the cache's type, heads side by side;
- *             rows of q 16-byte aligned.  out must not overlap q or the cache.
+ *             rows of q 16-byte aligned.  Rows of out overlap neither rows of q nor
+ *             the cache (MOE_ERR_ARG); both may be parts of the same longer rows.
  *   ws        device workspace of moe_tree_attention_plan's bytes for the same
  *             sizes (NULL when that is 0); scratch between calls.
  * Scores, softmax and sums are fp32; the softmax weights enter the second product

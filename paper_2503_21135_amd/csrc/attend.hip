@@ -596,12 +596,14 @@ extern "C" int moe_tree_attention(const moe_cache_t* C, const int32_t* table, in
   if (n_seqs == 0 || n_tokens == 0 || max_new == 0) return MOE_OK;
   if (int st = check_batch(C, table, max_pages, cache_len, new_off)) return st;
   const int64_t width = static_cast<int64_t>(n_q_heads) * C->head_dim;
-  if (!q || !out || q == out || ld_q < width || ld_out < width) return MOE_ERR_ARG;
+  if (!q || !out || ld_q < width || ld_out < width) return MOE_ERR_ARG;
   if (!aligned16(q) || ld_q % 8 || !aligned_to(out, 2) || !aligned_to(mask, 8)) return MOE_ERR_ALIGN;
   size_t need = 0;
   if (int st = moe_tree_attention_plan(C, n_q_heads, n_seqs, max_new, max_len, nullptr, &need)) return st;
   if (need > 0 && (!ws || ws_bytes < need)) return MOE_ERR_WORKSPACE;
   if (need > 0 && !aligned16(ws)) return MOE_ERR_ALIGN;
+  const Rows out_rows{out, n_tokens, 2 * width, 2 * ld_out};
+  if (overlap(out_rows, Rows{q, n_tokens, 2 * width, 2 * ld_q}) || over_cache(out_rows, C)) return MOE_ERR_ARG;
   const Plan p = plan_of(C, n_q_heads, n_seqs, max_new, max_len);
   // threads of a launch
   if (cdiv(static_cast<int64_t>(n_seqs) * C->n_heads * p.n_split, 8) * 8 * p.row_blocks * (p.row_waves == 1 ? 256 : 512) > UINT32_MAX)

@@ -61,6 +61,12 @@ inline int check_batch(const moe_cache_t* C, const int32_t* table, int32_t max_p
   return MOE_OK;
 }
 
+// Whether rows that a call writes share a byte with the cache's keys or values.
+inline bool over_cache(const Rows& out, const moe_cache_t* C) {
+  const int64_t bytes = static_cast<int64_t>(C->n_pages) * C->n_heads * C->page_size * C->head_dim * 2;
+  return overlap(out, Rows{C->k, 1, bytes, bytes}) || overlap(out, Rows{C->v, 1, bytes, bytes});
+}
+
 inline Batch batch_of(const moe_cache_t* C, const int32_t* table, int32_t max_pages, const int32_t* len,
                       int32_t n_seqs, const int32_t* off, int32_t n_tokens, int32_t max_new, int32_t* status) {
   return Batch{table, len, off, status, max_pages, n_seqs, n_tokens, max_new,

@@ -24,6 +24,30 @@ inline bool overlap(const void* p, int64_t n, const void* q, int64_t m) {
   return p && q && a < b + static_cast<uintptr_t>(m) && b < a + static_cast<uintptr_t>(n);
 }
 
+
+// Rows of a caller's array: n of them, each `bytes` long, `stride` bytes (>= bytes) apart.
+struct Rows {
+  const void* at;
+  int64_t n, bytes, stride;
+};
+// Whether a row of p shares a byte with a row of q.  Rows of one may lie between those of the
+// other (parts of one projection's rows).
+inline bool overlap(const Rows& p, const Rows& q) {
+  if (!overlap(p.at, (p.n - 1) * p.stride + p.bytes, q.at, (q.n - 1) * q.stride + q.bytes)) return false;
+  const int64_t d = static_cast<const char*>(q.at) - static_cast<const char*>(p.at);
+  if (p.stride == q.stride) {   // row j of q starts d + (j - i) stride behind row i of p
+    const int64_t lo = 1 - p.n, hi = q.n - 1;   // of j - i; rows meet where -q.bytes < d + (j - i) stride < p.bytes
+    const auto floor_div = [](int64_t x, int64_t y) { return x / y - (x % y < 0); };
+    const int64_t first = floor_div(-q.bytes - d, p.stride) + 1, last = floor_div(p.bytes - d - 1, p.stride);
+    return (first > lo ? first : lo) <= (last < hi ? last : hi);
+  }
+  for (int64_t i = 0; i < p.n; i++) {           // row j of q starts j * q.stride - x behind row i of p
+    const int64_t x = i * p.stride - d, j = x < q.bytes ? 0 : (x - q.bytes) / q.stride + 1;
+    if (j < q.n && j * q.stride - x < p.bytes) return true;
+  }
+  return false;
+}
+
 template <int TYPE> struct ElemOf;
 template <> struct ElemOf<MOE_TYPE_BF16> { typedef __bf16 type; };
 template <> struct ElemOf<MOE_TYPE_FP16> { typedef _Float16 type; };

@@ -18,3 +18,24 @@ def test_norm_outputs_over_gate_and_weights(lib):  # noqa: F811
                dict(gate=H, gt=1, **element),                                     # in place over another type
                dict(ro=R, gate=R + 2, **element), dict(ro=G, gate=G, gt=2, **element), dict(ro=W, w=W), dict(ro=W, wp=W)):
         assert call(**kw) == ARG, kw
+
+
+def cache_at(k, v):
+    """A cache of 8 pages, 2 heads of 64, 32 slots: 64 KB each for keys and values."""
+    from test_block_cpu import cache_desc
+    return cache_desc(k=k, v=v)
+
+
+K, V, Q = FAKE + (8 << 20), FAKE + (9 << 20), FAKE + (10 << 20)
+
+
+def test_attention_output_over_queries_and_cache(lib):  # noqa: F811
+    call = caller(lib.moe_tree_attention, dict(
+        c=cache_at(K, V), table=FAKE, pages=4, lens=FAKE, B=2, off=FAKE, N=6, mx=4, ml=64, q=Q, ldq=256, Hq=4, mask=None,
+        mw=0, scale=0.125, out=Q + (1 << 20), ldo=256, st=None, ws=None, wsb=0, stream=None))
+    for kw in (dict(out=Q + 2), dict(out=Q - 2), dict(out=Q + 512 * 5 + 510), dict(out=Q - 512 * 6 + 2),   # rows of 512 bytes
+               dict(ldq=512, ldo=512, out=Q + 256), dict(ldq=512, ldo=512, out=Q - 510),    # between rows, but too near
+               dict(ldq=512, out=Q + 512),                                   # strides that differ: rows meet further on
+               dict(N=1, B=1, ldq=4096, out=Q + 510),
+               dict(out=K), dict(out=K + 65534), dict(out=V - 512 * 6 + 2), dict(out=V + 100)):
+        assert call(**kw) == ARG, kw

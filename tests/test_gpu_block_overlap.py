@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from test_gpu_block import BF16, P, norm_case
+from test_gpu_block import BF16, P, batch, gen, norm_case
 
 pytestmark = pytest.mark.gpu
 
@@ -24,3 +24,23 @@ def test_norm_in_place_of_any_input(T, d):
             h = t[over_h] if over_h else torch.empty_like(t["r"])
             P().moe_block_norm(t["r"], h, y=t["y"], gate=t["gate"], r_out=r_out, **w)
             assert torch.equal(r_out, s["r_out"]) and torch.equal(h, s["h"]), (over_r, over_h)
+
+
+@pytest.mark.parametrize("ctx,new", [(0, 1), (90, 7), (4000, 40)])
+def test_attention_between_rows(ctx, new):
+    """Queries and outputs as parts of the same rows."""
+    cache, off = batch([ctx], [new], 32, 2, 64, BF16, 5)
+    q = torch.randn(new, 4, 64, device="cuda", generator=gen(6)).to(BF16)
+    want = cache.attend(q, off, new, ctx + new)
+    for q_at, o_at in ((0, 4), (4, 0), (5, 1)):
+        rows = torch.full((new, 10, 64), 3.0, device="cuda").to(BF16)
+        rows[:, q_at:q_at + 4] = q
+        before = rows.clone()
+        cache.attend(rows[:, q_at:q_at + 4], off, new, ctx + new, out=rows[:, o_at:o_at + 4])
+        assert torch.equal(rows[:, o_at:o_at + 4], want)
+        rows[:, o_at:o_at + 4] = before[:, o_at:o_at + 4]
+        assert torch.equal(rows, before)
+    rows = torch.zeros(2 * new + 2, 4, 64, device="cuda", dtype=BF16)   # one after the other in an allocation
+    rows[new:2 * new] = q
+    cache.attend(rows[new:2 * new], off, new, ctx + new, out=rows[:new])
+    assert torch.equal(rows[:new], want)
