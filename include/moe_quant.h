@@ -626,6 +626,8 @@ typedef struct moe_cache {
  *              pairs (c, c + rot_dim/2), or (2c, 2c + 1) when interleaved != 0:
  *              (a, b) -> (a cos - b sin, a sin + b cos), fp32, rounded once.
  *   q_out      device [n_tokens][ld_q_out], NULL when q is; may be q itself (same ld).
+ *              Its rows overlap no other rows of q, k and v and not the cache
+ *              (MOE_ERR_ARG).
  */
 int moe_cache_append(const moe_cache_t* C, const int32_t* table, int32_t max_pages,
                      const int32_t* cache_len, int32_t n_seqs, const int32_t* new_off,

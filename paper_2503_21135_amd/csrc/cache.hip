@@ -302,6 +302,13 @@ extern "C" int moe_cache_append(const moe_cache_t* C, const int32_t* table, int3
   if (!aligned_to(q, 2) || !aligned_to(k, 2) || !aligned_to(v, 2) || !aligned_to(q_out, 2) || !aligned_to(cos, 4) ||
       !aligned_to(sin, 4) || !aligned_to(positions, 4))
     return MOE_ERR_ALIGN;
+  if (q) {
+    const int64_t wide = 2 * static_cast<int64_t>(n_q_heads) * D, slim = 2 * static_cast<int64_t>(C->n_heads) * D;
+    const Rows out{q_out, n_tokens, wide, 2 * ld_q_out};
+    if ((q != q_out && overlap(out, Rows{q, n_tokens, wide, 2 * ld_q})) || overlap(out, Rows{k, n_tokens, slim, 2 * ld_k}) ||
+        overlap(out, Rows{v, n_tokens, slim, 2 * ld_v}) || over_cache(out, C))
+      return MOE_ERR_ARG;
+  }
   const AppendArgs a{batch_of(C, table, max_pages, cache_len, n_seqs, new_off, n_tokens, max_new, status),
                      q, k, v, q_out, C->k, C->v, positions, cos, sin, ld_q, ld_k, ld_v, ld_q_out,
                      n_q_heads / C->n_heads, rot_dim, max_pos, interleaved};

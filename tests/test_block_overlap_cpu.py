@@ -39,3 +39,12 @@ def test_attention_output_over_queries_and_cache(lib):  # noqa: F811
                dict(N=1, B=1, ldq=4096, out=Q + 510),
                dict(out=K), dict(out=K + 65534), dict(out=V - 512 * 6 + 2), dict(out=V + 100)):
         assert call(**kw) == ARG, kw
+
+
+def test_append_output_over_inputs_and_cache(lib):  # noqa: F811
+    call = caller(lib.moe_cache_append, dict(
+        c=cache_at(K, V), table=FAKE, pages=4, lens=FAKE, B=2, off=FAKE, N=6, mx=4, q=Q, ldq=512, Hq=4, k=Q + 512, ldk=512,
+        v=Q + 768, ldv=512, pos=None, cos=None, sin=None, rot=0, mp=0, il=0, qo=Q + (1 << 20), ldqo=256, st=None, stream=None))
+    for kw in (dict(qo=Q + 2, ldqo=512), dict(qo=Q + 16), dict(qo=Q + 512, ldqo=512), dict(qo=Q + 766, ldqo=512),
+               dict(qo=Q - 2, ldqo=512), dict(qo=K), dict(qo=V + 65534), dict(qo=V - 512 * 6 + 2)):
+        assert call(**kw) == ARG, kw

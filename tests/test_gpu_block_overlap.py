@@ -44,3 +44,26 @@ def test_attention_between_rows(ctx, new):
     rows[new:2 * new] = q
     cache.attend(rows[new:2 * new], off, new, ctx + new, out=rows[:new])
     assert torch.equal(rows[:new], want)
+
+
+@pytest.mark.parametrize("q_out", ["in place", "beside"])
+def test_append_between_rows(q_out):
+    """Queries, keys, values and rotated queries as parts of the same rows."""
+    new, Hq, Hkv, D = [5, 70], 4, 2, 64
+    cache, off = batch([33, 0], new, 32, Hkv, D, BF16, 7)
+    rows = torch.randn(75, 2 * Hq + 2 * Hkv, D, device="cuda", generator=gen(8)).to(BF16)
+    ang = torch.rand(200, D // 2, device="cuda", generator=gen(9)) * 6.28
+    rot = dict(cos=ang.cos(), sin=ang.sin())
+    q, k, v = rows[:, :Hq], rows[:, Hq:Hq + Hkv], rows[:, Hq + Hkv:Hq + 2 * Hkv]
+    want = cache.append(q, k, v, off, 70, **rot)
+    kept = cache.k.clone(), cache.v.clone()
+    cache.k.zero_(), cache.v.zero_()
+    cache.append(q, k, v, off, 70, q_out=q if q_out == "in place" else rows[:, Hq + 2 * Hkv:], **rot)
+    assert torch.equal(q if q_out == "in place" else rows[:, Hq + 2 * Hkv:], want)
+    for b in range(2):
+        for a, w in zip((cache.k, cache.v), kept):
+            n = [33, 0][b]
+            for slot in range(n, n + new[b]):
+                pg, o = int(cache.table[b, slot // 32]), slot % 32
+                at = (pg, slice(None), o) if a is cache.k else (pg, slice(None), slice(None), o)
+                assert torch.equal(a[at], w[at])
