@@ -685,7 +685,8 @@ int moe_tree_attention(const moe_cache_t* C, const int32_t* table, int32_t max_p
  * cache_len[b] + j.  A list that is not ascending or names a token the sequence
  * does not have moves nothing (MOE_ERR_SLOT in status).
  *   len_out   device int32 [n_seqs] or NULL: cache_len[b] + n_keep[b] (cache_len[b]
- *             where nothing moves for a bad list); must not be cache_len itself.
+ *             where nothing moves for a bad list); overlaps neither cache_len nor
+ *             another input nor the cache (MOE_ERR_ARG).
  */
 int moe_cache_keep(const moe_cache_t* C, const int32_t* table, int32_t max_pages,
                    const int32_t* cache_len, int32_t n_seqs, const int32_t* new_off,

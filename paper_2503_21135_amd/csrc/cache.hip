@@ -330,8 +330,15 @@ extern "C" int moe_cache_keep(const moe_cache_t* C, const int32_t* table, int32_
   if (n_seqs < 0 || n_seqs > 65535 || max_keep < 0) return MOE_ERR_ARG;
   if (n_seqs == 0) return MOE_OK;
   if (int st = check_batch(C, table, max_pages, cache_len, new_off)) return st;
-  if (!n_keep || (max_keep > 0 && !keep) || len_out == cache_len) return MOE_ERR_ARG;
+  if (!n_keep || (max_keep > 0 && !keep)) return MOE_ERR_ARG;
   if (!aligned_to(keep, 4) || !aligned_to(n_keep, 4) || !aligned_to(len_out, 4)) return MOE_ERR_ALIGN;
+  if (len_out) {   // written by one workgroup of a sequence while others still read
+    const int64_t bytes = 4 * static_cast<int64_t>(n_seqs);
+    if (overlap(len_out, bytes, cache_len, bytes) || overlap(len_out, bytes, new_off, bytes + 4) ||
+        overlap(len_out, bytes, n_keep, bytes) || overlap(len_out, bytes, keep, bytes * max_keep) ||
+        overlap(len_out, bytes, table, bytes * max_pages) || over_cache(Rows{len_out, 1, bytes, bytes}, C))
+      return MOE_ERR_ARG;
+  }
   const KeepArgs a{batch_of(C, table, max_pages, cache_len, n_seqs, new_off, INT32_MAX, INT32_MAX, status),
                    C->k, C->v, keep, n_keep, len_out, max_keep};
   hipStream_t s = static_cast<hipStream_t>(stream);

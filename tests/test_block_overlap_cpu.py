@@ -48,3 +48,11 @@ def test_append_output_over_inputs_and_cache(lib):  # noqa: F811
     for kw in (dict(qo=Q + 2, ldqo=512), dict(qo=Q + 16), dict(qo=Q + 512, ldqo=512), dict(qo=Q + 766, ldqo=512),
                dict(qo=Q - 2, ldqo=512), dict(qo=K), dict(qo=V + 65534), dict(qo=V - 512 * 6 + 2)):
         assert call(**kw) == ARG, kw
+
+
+def test_keep_lengths_over_inputs(lib):  # noqa: F811
+    call = caller(lib.moe_cache_keep, dict(c=cache_at(K, V), table=Q, pages=4, lens=FAKE, B=3, off=G, keep=W, mk=4, n=H, lo=R + 512,
+                                           st=None, stream=None))
+    for kw in (dict(lo=FAKE + 8), dict(lo=FAKE - 8), dict(lo=G + 12), dict(lo=H + 4), dict(lo=W + 44), dict(lo=Q + 40),
+               dict(lo=K), dict(lo=V + 65532)):
+        assert call(**kw) == ARG, kw
