@@ -119,7 +119,7 @@ def main():
     out, steps = decode(model, prompt, 60)
     want = decode_plain(plain, prompt, 60)
     same = sum(a == b for a, b in zip(out, want))
-    assert all(c.status_value() == 0 for c in model.caches + plain.caches)
+    assert all(x.status_value() == 0 for m in (model, plain) for x in m.caches + m.blocks)
     print("%d tokens in %d steps of the model; %d of them as one token at a time gives" % (len(out), steps, same))
     return out, want, steps
 

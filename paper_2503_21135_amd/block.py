@@ -189,6 +189,12 @@ class DecoderBlock:
         self.cos, self.sin = cos, sin
         self.scales = dict(residual_scale=residual_scale, branch_scale=branch_scale)
 
+    def status_value(self) -> int:
+        """0, or MOE_ERR_RANGE once the expert layer, whose operands are fp16 for many tokens,
+        has met a value beyond fp16's range: that call's outputs are not valid.  Reads it
+        back.  (What the cache has met is in its own status_value.)"""
+        return self.moe.ffn_status_value()
+
     def attention(self, h: torch.Tensor, cache: PagedCache, new_off: torch.Tensor, max_new: int, max_len: int,
                   positions: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
                   stream=None) -> torch.Tensor:

@@ -1,4 +1,5 @@
-"""The decoder block's classes on several streams and in several captured graphs.
+"""The decoder block's classes on several streams, in several captured graphs and over many
+batch sizes.
 
 Nothing that would race is launched: what two calls that may run side by side are given to
 work in is compared first."""
@@ -79,7 +80,7 @@ class Request:
 
     def __init__(self, block, d, T, seed, ctx=30):
         self.block, self.T = block, T
-        self.cache = P().PagedCache.create(1, 256, block.Hkv, block.D, page_size=32)
+        self.cache = P().PagedCache.create(1, ctx + T, block.Hkv, block.D, page_size=32)
         self.cache.k.copy_(torch.randn(self.cache.k.shape, device="cuda", generator=gen(seed)))
         self.cache.v.copy_(torch.randn(self.cache.v.shape, device="cuda", generator=gen(seed + 1)))
         self.cache.lens.fill_(ctx)
@@ -212,3 +213,15 @@ def test_block_memory_stays_bounded_over_many_sizes():
     del first, again
     held = torch.cuda.memory_allocated() - before
     assert held <= 4 * largest, "%d bytes held, a batch of the largest size needs %d" % (held, largest)
+
+
+@pytest.mark.parametrize("T,size,code", [(24, 1e6, 0), (700, 1.0, 0), (700, 1e6, -6)])
+def test_block_tells_of_values_past_the_expert_layers_range(T, size, code):
+    """Few tokens take any bf16 activation; many, whose operands are fp16, say so when one is
+    beyond 65504 (a norm weight of 10^6 makes some)."""
+    block, d = small_block(80)
+    block.norms = dict(block.norms, ffn=torch.full((d,), size, device="cuda"))
+    Request(block, d, T, 400).step()
+    assert block.status_value() == code
+    block.moe.clear_ffn_status()
+    assert block.status_value() == 0
