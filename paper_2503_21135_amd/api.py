@@ -241,9 +241,9 @@ def moe_quant_linear(x: torch.Tensor, codes: torch.Tensor, sz: torch.Tensor, y: 
     xp, ld_x = _rows(x, T, K, "x")
     cp, ld_c = _rows(codes, R, words, "codes")
     yp, ld_y = _rows(y, T, R, "y")
-    st = load().moe_quant_linear(xp, _type(x, "x"), ld_x, T, K, cp, ld_c, sz.data_ptr(), sr if R > 1 else 1,
-                                 sg if G > 1 else R, R, bits, K // G, _flat(bias, (R,), torch.float32, "bias"),
-                                 yp, _type(y, "y"), ld_y, _stream(stream, x))
+    st = load().moe_quant_linear(xp, _type(x, "x"), ld_x, T, K, cp, ld_c if R > 1 else K // 8,
+                                 sz.data_ptr(), sr if R > 1 else 1, sg if G > 1 else R, R, bits, K // G,
+                                 _flat(bias, (R,), torch.float32, "bias"), yp, _type(y, "y"), ld_y, _stream(stream, x))
     if st:
         check(st, "moe_quant_linear")
 
