@@ -96,6 +96,12 @@ __global__ void __launch_bounds__(RW == 1 ? 256 : 512, D <= 128 || RW > 1 ? 2 : 
   constexpr int NC = D / 32, NV = D / 16, W = RW == 1 ? 4 : 8, KW = W / RW;
   // tiles that a key group stages at once (with one, 204 us where two take 190, four 196),
   // threads of a key group, and their 16-byte pieces of a stage's keys
+  // The second product takes weights as operands of the cache's type.  Few rows, which wait for
+  // HBM, add the product with what that rounding left over, so that the output's error is its own
+  // rounding's (64 x 1 over 4096, bf16: 1.7e-3 against 64 bits, else 2.3e-3) at the same time
+  // (161.2 us both ways; 16 x 4 drafts of 8 heads over 2000 13.3 instead of 12.9).  Many rows would
+  // pay for it: 4 x 64 over 32768 206 us instead of 156, 8 x 32 over 8000 79 instead of 71.
+  constexpr bool kRest = RW == 1;
   constexpr int KT = RW == 1 ? 1 : std::min(2, RW * 64 / D), TG = RW * kWave, NP = KT * 4 * D / TG;
   struct Tile {
     u32x4 k[kTile][D / 8];    // row 16 kt + col is the operand row of lane col in tile kt; pieces and rows are
@@ -189,7 +195,7 @@ __global__ void __launch_bounds__(RW == 1 ? 256 : 512, D <= 128 || RW > 1 ? 2 : 
 #pragma unroll
         for (int rt = 0; rt < RT; rt++) sc[rt][kt] = product<TYPE>(k, qf[rt][c], c ? sc[rt][kt] : f32x4{0.f, 0.f, 0.f, 0.f});
       }
-    u32x4 pf[RT];
+    u32x4 pf[RT], rest[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; rt++) {
       float x[8], y[8];
@@ -233,6 +239,13 @@ __global__ void __launch_bounds__(RW == 1 ? 256 : 512, D <= 128 || RW > 1 ? 2 : 
       // outweighs the rest cancels
 #pragma unroll
       for (int i = 0; i < 4; i++) l[rt] = dot2<TYPE>(pf[rt][i], kOnes<TYPE>, l[rt]);
+      if constexpr (kRest) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+          rest[rt][i] = pack2<TYPE>(p[2 * i] - half_lo<TYPE>(pf[rt][i]), p[2 * i + 1] - half_hi<TYPE>(pf[rt][i]));
+          l[rt] = dot2<TYPE>(rest[rt][i], kOnes<TYPE>, l[rt]);
+        }
+      }
     }
     const int valid = min(max(total - j0, 0), 8);
     const uint32_t scrub = RW > 1 && t < t_full ? 0u : 0xFFFFFFFFu;   // a stage's edge may be behind this tile of it
@@ -248,7 +261,10 @@ __global__ void __launch_bounds__(RW == 1 ? 256 : 512, D <= 128 || RW > 1 ? 2 : 
           odd |= bad;
         }
 #pragma unroll
-      for (int rt = 0; rt < RT; rt++) o[rt][v] = product<TYPE>(w, pf[rt], o[rt][v]);
+      for (int rt = 0; rt < RT; rt++) {
+        o[rt][v] = product<TYPE>(w, pf[rt], o[rt][v]);
+        if constexpr (kRest) o[rt][v] = product<TYPE>(w, rest[rt], o[rt][v]);
+      }
     }
   };
 

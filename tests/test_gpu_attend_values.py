@@ -6,7 +6,7 @@ import math
 import pytest
 import torch
 
-from test_gpu_block import BF16, FP16, P, batch, gen, within
+from test_gpu_block import BF16, E32, FP16, P, TINY, U, batch, gen, rows_of, within
 
 pytestmark = pytest.mark.gpu
 
@@ -61,3 +61,31 @@ def test_many_small_weights_count(D, new):
     for guess in (0, N + new):             # the keys in one part, and in many
         out = cache.attend(q, off, new, guess, scale=26.5 * math.log(2) / 16)
         within(out, want, bound, "small weights")
+
+
+@pytest.mark.parametrize("lens,new,Hq,Hkv,D,dt", [
+    ([100], [1], 4, 2, 64, BF16), ([700, 33], [3, 1], 8, 2, 64, FP16), ([2500], [4], 16, 2, 64, BF16),
+    ([0, 31], [8, 2], 4, 1, 128, BF16), ([3000, 5], [1, 1], 8, 2, 128, BF16), ([900], [32], 2, 2, 128, FP16),
+    ([64], [1], 16, 1, 256, BF16), ([1200, 7], [4, 3], 4, 1, 256, FP16)])
+def test_few_rows_keep_more_of_their_weights(lens, new, Hq, Hkv, D, dt):
+    """Up to 32 rows per key head (16 at head_dim 256) a weight is off by 2^-16 of itself, its
+    exponential's error included, or by 2^-32 of the largest where fp16 cannot hold its rest;
+    scores as in attention_want.  The output's rounding is the largest error then."""
+    cache, off = batch(lens, new, 32, Hkv, D, dt, 23)
+    q = torch.randn(sum(new), Hq, D, device="cuda", generator=gen(24)).to(dt)
+    out = cache.attend(q, off, max(new), max(a + n for a, n in zip(lens, new)))
+    scale, n0 = D ** -0.5, 0
+    for b, (a, n) in enumerate(zip(lens, new)):
+        for i in range(n):
+            seen = a + i + 1
+            k, v = (x.double() for x in rows_of(cache, b, range(seen)))
+            qi = q[n0 + i].double().view(Hkv, -1, D)
+            k, v = k.permute(1, 2, 0).contiguous(), v.transpose(0, 1).contiguous()
+            w = torch.softmax(torch.matmul(qi, k) * scale, 2)
+            e = (D + 8) * E32 * scale * torch.matmul(qi.abs(), k.abs()).amax(2, keepdim=True)
+            want, size = torch.matmul(w, v), torch.matmul(w, v.abs())
+            rel = 4 * e + 2 * 2.0 ** -16 + (seen / 16 + 64) * E32
+            bound = rel * size + (2 * 2.0 ** -32 * v.abs().sum(1, keepdim=True) if dt == FP16 else 0)
+            bound = bound + U[dt] * 1.01 * want.abs() + TINY[dt]
+            within(out[n0 + i].view(Hkv, -1, D), want, bound, "sequence %d, token %d" % (b, i))
+        n0 += n
