@@ -81,20 +81,23 @@ __device__ __forceinline__ uint32_t seen8(const AttendArgs& a, int64_t t, int i,
 // barrier a stage).  Straight from memory an operand has 16 rows side by side, whose
 // 16-byte pieces the vector memory path serves one per cycle: enough for one wave per tile
 // to keep up with HBM, not for several on the same one (64 drafts by 4 heads per key head
-// over 4 x 32768 slots: 310 us that way, 174 this way).
+// over 4 x 32768 slots: 448 us that way, 156 this way, the join included).
 //
-// Few rows are bound by HBM: 64 sequences of one token over up to 4096, 778 MB, 157 us and
-// 4.5 to join, 4.8 TB/s.  At 256 rows per key head (4 x 64 drafts over 32768, 88 GFLOP,
-// 418 MB: 180 us and 9 to join) a tile's matrix instructions (1024 cycles of each SIMD), vector
-// instructions (1100) and LDS reads (1150) follow each other rather than overlap, and
-// shorter sequences end before the longest.  Giving one wave of a SIMD the higher priority,
-// or the waves in their matrix instructions, left that as it was, and so did reading the
-// value operands before the softmax and four tiles a stage.
+// Few rows are bound by HBM: 64 sequences of one token over up to 4096, 778 MB, 155 us and
+// 4.8 to join, 5.0 TB/s.  At 256 rows per key head (4 x 64 drafts over up to 32768, 88 GFLOP,
+// 418 MB: 148 us and 7.8 to join; 193 and 9 on a card that has rested) a tile's matrix
+// instructions (1024 cycles of each SIMD), vector instructions (1100) and LDS reads (1150)
+// follow each other rather than overlap: matrix instructions fill 39 % of a busy CU's
+// cycles.  And parts are uneven: of lengths from 18706 to 32768 they make 208 workgroups
+// of up to 129 tiles, where an even share of 256 CUs is 99, and parts of one number fall on
+// one XCD.  Giving one wave of a SIMD the higher priority, or the waves in their matrix
+// instructions, left that as it was, and so did reading the value operands before the softmax.
 template <int TYPE, int D, int RT, int RW>
 __global__ void __launch_bounds__(RW == 1 ? 256 : 512, D <= 128 || RW > 1 ? 2 : 1) attend_kernel(AttendArgs a) {
   typedef elem_t<TYPE> E;
   constexpr int NC = D / 32, NV = D / 16, W = RW == 1 ? 4 : 8, KW = W / RW;
-  // tiles that a key group stages at once (with one, 204 us where two take 190, four 196),
+  // tiles that a key group stages at once (4 x 64 over 32768: one 159 us, two 161, four 169;
+  // head_dim 64 over 8000: two 39, four 42, and one would leave threads without a piece),
   // threads of a key group, and their 16-byte pieces of a stage's keys
   // The second product takes weights as operands of the cache's type.  Few rows, which wait for
   // HBM, add the product with what that rounding left over, so that the output's error is its own
@@ -518,9 +521,9 @@ __global__ void __launch_bounds__(256) join_kernel(AttendArgs a) {
 // How a batch is laid over workgroups.  Up to 16 rows (32 where the registers allow two
 // tiles) per key head go straight from memory, more through LDS with as many row waves as
 // it takes.  Parts: enough for 1024 workgroups straight from memory (four a CU), 256 through LDS
-// (one a CU; with 512, which run one after another, the large trees take 190 us instead
-// of 174, 2 x 32 drafts over 16000 51 instead of 40, 4 x 12 of head_dim 256 over 4000 30
-// instead of 20), and no shorter than two steps of every wave.
+// (one a CU; with 512, which run one after another, the large trees take 176 us instead
+// of 160, 2 x 32 drafts over 16000 60 instead of 47, 4 x 12 of head_dim 256 over 4000 36
+// instead of 26, joins included), and no shorter than two steps of every wave.
 struct Plan {
   int row_waves;   // RW of the kernel
   int row_tiles;   // 16-row tiles of a wave

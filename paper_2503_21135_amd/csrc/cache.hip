@@ -31,7 +31,7 @@ struct __attribute__((packed, aligned(2))) Piece { uint32_t w[4]; };
 // the page's [channel][slot] rows, 8 slots to a store.  Bound by HBM where there are
 // many tokens, each row being read and written once (8192 tokens of 32 + 2 x 8 heads of
 // 128, 206 MB: 51 us, 4.0 TB/s), else by its four dependent loads (one token 5.0 us, 32
-// trees of 16 to 32 tokens 12.2 us).  4 D threads give each thread one pair of chunks of
+// trees of 16 to 32 tokens 11.9 us).  4 D threads give each thread one pair of chunks of
 // one token: with 256, which take two passes at D = 128, the trees take 14.9 us, one token
 // 7.6, the prompt 49.
 template <int TYPE, int D>
@@ -194,7 +194,7 @@ struct KeepArgs {
 // before any is written; indices ascend, so no later row's source is written before
 // it is read.  Rows that stay where they are are left alone.  The transposed values make
 // a moved row touch head_dim cache lines, which is what bounds a large batch (256
-// sequences of 8 heads of 128, 12.8 MB of rows: 15.9 us; one sequence 3.8 us); 8 rows side
+// sequences of 8 heads of 128, 12.8 MB of rows: 16 to 19 us; one sequence 3.6 us); 8 rows side
 // by side share those lines (with channels side by side: 24.7 us).
 template <int D>
 __global__ void __launch_bounds__(kThreads) keep_kernel(KeepArgs a) {

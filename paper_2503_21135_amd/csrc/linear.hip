@@ -51,7 +51,7 @@ __device__ __forceinline__ void store_y(const LinearArgs& a, int t, int r, float
 // One token, and two by few rows: a wave takes RW rows, its lanes side by side along K, 32 codes
 // each; no LDS and no barrier.  The activations' shares and their sums stay in registers
 // for all rows of a step.  Bound by HBM where there are many rows (one token by 32000 x
-// 4096, 70 MB: 15.8 us, 4.4 TB/s), else by the chain of loads (4096 x 4096: 4.5 us).
+// 4096, 70 MB: 15.0 us, 4.6 TB/s), else by the chain of loads (4096 x 4096: 4.4 us).
 constexpr int kVecWaves = 4;
 
 template <int TYPE, int T, int RW>
@@ -126,11 +126,11 @@ __global__ void __launch_bounds__(kVecWaves * kWave) linear_vec_kernel(LinearArg
 // barrier a step; the next step's activations and codes are on their way during the
 // products.
 //
-// 64 tokens by 32000 x 4096 (78 MB, 16.8 GFLOP) take 34.6 us; the vector instructions
+// 64 tokens by 32000 x 4096 (78 MB, 16.8 GFLOP) take 33.1 us; the vector instructions
 // (unpacking, scale and zero point, staging: 278 per wave and step beside 32 matrix
 // instructions) fill about half of the issue slots, the waits around the barrier most of
 // the rest.  Prefetching codes four steps ahead, activations two, or the LDS operands one
-// product ahead changed nothing (37.3, 37.3 and 35.6 us against 37.2 and 35.1).
+// product ahead changed nothing (37.3, 37.3 and 35.6 us against 37.2 and 35.1, on a card that had rested).
 //
 // A lane's four code words are turned across the four lane groups (four half-swaps),
 // which puts word 4m + g into group g: k = 32m + 8g .. + 7, the activations' own order.
@@ -275,8 +275,9 @@ __global__ void __launch_bounds__(W * kWave) linear_tile_kernel(LinearArgs a) {
   }
 }
 
-// Two rows a wave until four fill the machine (one token, us: 4096 rows 4.4 against 4.9,
-// 32000 rows 16.2 against 15.1).
+// Two rows a wave while rows are few, four where there are many (one token, us, two and four:
+// 4096 rows 4.3 and 4.7, 9000 6.6 and 7.3, 16000 9.0 and 9.4, 32000 15.0 and 15.0, 128000 71.3
+// and 69.1).
 template <int TYPE, int T, int RW>
 void launch_vec(const LinearArgs& a, hipStream_t s) {
   hipLaunchKernelGGL((linear_vec_kernel<TYPE, T, RW>), dim3(static_cast<unsigned>(cdiv(a.R, kVecWaves * RW))), dim3(kVecWaves * kWave),
@@ -296,6 +297,8 @@ void launch_tile(const LinearArgs& a, hipStream_t s) {
 //   37 tokens   6144 rows: 32 a workgroup 14.3, 64 16.1
 //   16 tokens   6144 rows: 16 a workgroup 8.8, 32 9.0, 64 10.0;  32000: 32 18.5, 64 15.9, 128 17.9
 //   5 tokens    4096 rows: 16 a workgroup 6.0, 32 7.4, 64 8.8
+// (each line taken together, on a card that had rested; after some hundred calls the chosen
+// ones take 16.0, 18.0, 32.0; 12.5; 8.2, 15.4; 5.9)
 template <int TYPE, int GROUP, int NT>
 void launch_tile(const LinearArgs& a, hipStream_t s) {
   if (a.R > 8192) {
@@ -318,8 +321,8 @@ void launch_tiles(const LinearArgs& a, hipStream_t s) {
   }
 }
 
-// Two tokens take dot products while rows are few (us: 4096 rows 5.6, matrix tiles 6.0;
-// 32000 rows 20.6 and 16.2).
+// Two tokens take dot products while rows are few (us, taken together on a card that had
+// rested: 4096 rows 5.6, matrix tiles 6.0; 32000 rows 20.6 and 16.2).
 template <int TYPE>
 void launch_linear(const LinearArgs& a, hipStream_t s) {
   if (a.T == 1 && a.R <= 8192) launch_vec<TYPE, 1, 2>(a, s);

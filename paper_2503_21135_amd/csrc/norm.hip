@@ -105,7 +105,7 @@ __device__ __forceinline__ float row_sum(float v, float* part) {
 
 // TPR threads per row, NCH chunks of 8 channels per thread: the row is read once and
 // stays in registers across both norms, each channel with the thread that writes it.
-// Bound by HBM: 8192 rows of 2048 with every input (168 MB) take 34.9 us, 4.8 TB/s, the
+// Bound by HBM: 8192 rows of 2048 with every input (168 MB) take 36 us, 4.7 TB/s, the
 // rate of a large copy; one row of 256 takes 2.8 us.
 template <int TPR, int NCH>
 __global__ void __launch_bounds__(TPR < kNormThreads ? kNormThreads : TPR) norm_rows_kernel(NormArgs a) {
@@ -242,7 +242,7 @@ void launch_rows(const NormArgs& a, hipStream_t s) {
 }
 
 // As many threads as the row has chunks, so that each holds one: more chunks per thread
-// mean fewer waves to hide the loads.  us, rows x channels: 8192 x 2048 with 256 threads
+// mean fewer waves to hide the loads.  us, rows x channels, each pair taken together: 8192 x 2048 with 256 threads
 // 34.9, with one wave of four chunks 44.5; 4096 x 4096 with 512 threads 37.3, with 256 of
 // two chunks 37.7, 64 x 4096 4.5 and 6.3; 2048 x 8192 with 1024 threads 39.4, with 256 of
 // four chunks 44.7.  Up to 1024 channels a wave of its own spares a row the barriers where
