@@ -667,7 +667,7 @@ int moe_tree_attention_plan(const moe_cache_t* C, int32_t n_q_heads, int32_t n_s
  * Scores, softmax and sums are fp32.  The softmax weights enter the second product
  * and their own sum as matrix operands: rounded to the cache's type, or, up to 32
  * rows per key/value head (max_new * n_q_heads / n_heads; 16 at head_dim 256), as a
- * rounded weight and the rounded rest, 2^-16 of it at most left out.  (In fp16 a
+ * rounded weight and the rounded rest, 2^-15 of it at most left out.  (In fp16 a
  * weight below 2^-32 of the row's largest may count as zero.)  n_q_heads is a
  * multiple of n_heads, at most 64 times it; n_seqs * max_new * n_q_heads at most
  * 2^25.  Results are bitwise reproducible.

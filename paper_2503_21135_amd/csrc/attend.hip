@@ -47,6 +47,19 @@ __device__ __forceinline__ int tiles_per_part(const AttendArgs& a, int tiles) {
   return (tiles + parts - 1) / max(parts, 1);
 }
 
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+// Two weights rounded to a 16-bit type toward zero and one unit further, 0 staying 0: what is
+// left over is positive wherever the weight is, so that neither of the two products of an
+// infinite value has another sign or is NaN.
+template <int TYPE>
+__device__ __forceinline__ uint32_t below2(float a, float b) {
+  uint32_t w;
+  if constexpr (TYPE == MOE_TYPE_BF16) w = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+  else w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b));
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, w), u16x2{1, 1}));
+}
+
 // halves of w that are infinite or NaN, as 0xFFFF each
 template <int TYPE>
 __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
@@ -96,15 +109,15 @@ template <int TYPE, int D, int RT, int RW>
 __global__ void __launch_bounds__(RW == 1 ? 256 : 512, D <= 128 || RW > 1 ? 2 : 1) attend_kernel(AttendArgs a) {
   typedef elem_t<TYPE> E;
   constexpr int NC = D / 32, NV = D / 16, W = RW == 1 ? 4 : 8, KW = W / RW;
+  // The second product takes weights as operands of the cache's type.  Few rows, which wait for
+  // HBM, add the product with what a rounding down left over, so that the output's error is its own
+  // rounding's (64 x 1 over 4096, bf16: 1.7e-3 against 64 bits, else 2.3e-3) at the same time
+  // (160.1 us both ways; 64 x 8 drafts of head_dim 64 over 2000 58.3 instead of 57.8).  Many rows would
+  // pay for it: 4 x 64 over 32768 206 us instead of 156, 8 x 32 over 8000 79 instead of 71.
+  constexpr bool kRest = RW == 1;
   // tiles that a key group stages at once (4 x 64 over 32768: one 159 us, two 161, four 169;
   // head_dim 64 over 8000: two 39, four 42, and one would leave threads without a piece),
   // threads of a key group, and their 16-byte pieces of a stage's keys
-  // The second product takes weights as operands of the cache's type.  Few rows, which wait for
-  // HBM, add the product with what that rounding left over, so that the output's error is its own
-  // rounding's (64 x 1 over 4096, bf16: 1.7e-3 against 64 bits, else 2.3e-3) at the same time
-  // (161.2 us both ways; 16 x 4 drafts of 8 heads over 2000 13.3 instead of 12.9).  Many rows would
-  // pay for it: 4 x 64 over 32768 206 us instead of 156, 8 x 32 over 8000 79 instead of 71.
-  constexpr bool kRest = RW == 1;
   constexpr int KT = RW == 1 ? 1 : std::min(2, RW * 64 / D), TG = RW * kWave, NP = KT * 4 * D / TG;
   struct Tile {
     u32x4 k[kTile][D / 8];    // row 16 kt + col is the operand row of lane col in tile kt; pieces and rows are
@@ -237,17 +250,18 @@ __global__ void __launch_bounds__(RW == 1 ? 256 : 512, D <= 128 || RW > 1 ? 2 : 
         p[e] = __builtin_amdgcn_exp2f(y[e]);
         if constexpr (EDGE) p[e] = see >> e & 1 ? p[e] : 0.f;
       }
-      pf[rt] = u32x4{pack2<TYPE>(p[0], p[1]), pack2<TYPE>(p[2], p[3]), pack2<TYPE>(p[4], p[5]), pack2<TYPE>(p[6], p[7])};
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        const float a = p[2 * i], b = p[2 * i + 1];
+        pf[rt][i] = kRest ? below2<TYPE>(a, b) : pack2<TYPE>(a, b);
+        if constexpr (kRest) rest[rt][i] = pack2<TYPE>(a - half_lo<TYPE>(pf[rt][i]), b - half_hi<TYPE>(pf[rt][i]));
+      }
       // the sum is that of the rounded weights, so that what rounding does to a weight that
       // outweighs the rest cancels
 #pragma unroll
-      for (int i = 0; i < 4; i++) l[rt] = dot2<TYPE>(pf[rt][i], kOnes<TYPE>, l[rt]);
-      if constexpr (kRest) {
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-          rest[rt][i] = pack2<TYPE>(p[2 * i] - half_lo<TYPE>(pf[rt][i]), p[2 * i + 1] - half_hi<TYPE>(pf[rt][i]));
-          l[rt] = dot2<TYPE>(rest[rt][i], kOnes<TYPE>, l[rt]);
-        }
+      for (int i = 0; i < 4; i++) {
+        l[rt] = dot2<TYPE>(pf[rt][i], kOnes<TYPE>, l[rt]);
+        if constexpr (kRest) l[rt] = dot2<TYPE>(rest[rt][i], kOnes<TYPE>, l[rt]);
       }
     }
     const int valid = min(max(total - j0, 0), 8);

@@ -68,9 +68,9 @@ def test_many_small_weights_count(D, new):
     ([0, 31], [8, 2], 4, 1, 128, BF16), ([3000, 5], [1, 1], 8, 2, 128, BF16), ([900], [32], 2, 2, 128, FP16),
     ([64], [1], 16, 1, 256, BF16), ([1200, 7], [4, 3], 4, 1, 256, FP16)])
 def test_few_rows_keep_more_of_their_weights(lens, new, Hq, Hkv, D, dt):
-    """Up to 32 rows per key head (16 at head_dim 256) a weight is off by 2^-16 of itself, its
-    exponential's error included, or by 2^-32 of the largest where fp16 cannot hold its rest;
-    scores as in attention_want.  The output's rounding is the largest error then."""
+    """Up to 32 rows per key head (16 at head_dim 256) a weight, and so their sum, is off by 2^-15
+    of itself, its exponential's error included, or by 2^-32 of the largest where fp16 cannot
+    hold its rest; scores as in attention_want.  The output's rounding is the largest error then."""
     cache, off = batch(lens, new, 32, Hkv, D, dt, 23)
     q = torch.randn(sum(new), Hq, D, device="cuda", generator=gen(24)).to(dt)
     out = cache.attend(q, off, max(new), max(a + n for a, n in zip(lens, new)))
@@ -84,8 +84,35 @@ def test_few_rows_keep_more_of_their_weights(lens, new, Hq, Hkv, D, dt):
             w = torch.softmax(torch.matmul(qi, k) * scale, 2)
             e = (D + 8) * E32 * scale * torch.matmul(qi.abs(), k.abs()).amax(2, keepdim=True)
             want, size = torch.matmul(w, v), torch.matmul(w, v.abs())
-            rel = 4 * e + 2 * 2.0 ** -16 + (seen / 16 + 64) * E32
+            rel = 4 * e + 2 * 2.0 ** -15 + (seen / 16 + 64) * E32
             bound = rel * size + (2 * 2.0 ** -32 * v.abs().sum(1, keepdim=True) if dt == FP16 else 0)
             bound = bound + U[dt] * 1.01 * want.abs() + TINY[dt]
             within(out[n0 + i].view(Hkv, -1, D), want, bound, "sequence %d, token %d" % (b, i))
         n0 += n
+
+
+@pytest.mark.parametrize("D,new,Hq,dt", [
+    (64, 1, 4, BF16), (64, 7, 4, FP16), (64, 40, 4, BF16), (128, 3, 4, FP16), (128, 8, 4, BF16), (128, 60, 4, FP16),
+    (256, 2, 4, BF16), (256, 3, 5, FP16), (256, 40, 4, BF16)])
+@pytest.mark.parametrize("val", [math.inf, -math.inf])
+def test_infinite_cached_values_keep_their_sign(D, new, Hq, dt, val):
+    """Weights are positive (scores here are a few units apart), so one infinite value makes
+    its channel infinite for everybody, and two of opposite sign make it NaN."""
+    ctx, page = 500, 32
+    cache, off = batch([ctx], [new], page, 1, D, dt, 27)
+    q = torch.randn(new, Hq, D, device="cuda", generator=gen(28)).to(dt)
+    clean = cache.attend(q, off, new, ctx + new)
+    rest = [c for c in range(D) if c not in (3, 5)]
+    for tile in range(0, (ctx + page - 1) // page):
+        saved = cache.v.clone()
+        slot = tile * 32 + tile % 20
+        pg, o = int(cache.table[0, slot // page]), slot % page
+        cache.v[pg, 0, 3, o] = val
+        cache.v[pg, 0, 5, o] = val
+        far = (slot + 200) % ctx
+        cache.v[int(cache.table[0, far // page]), 0, 5, far % page] = -val
+        out = cache.attend(q, off, new, ctx + new)
+        cache.v.copy_(saved)
+        assert (out[:, :, 3] == val).all(), tile
+        assert torch.isnan(out[:, :, 5]).all(), tile
+        assert torch.equal(out[:, :, rest], clean[:, :, rest]), tile
