@@ -511,7 +511,8 @@ int moe_allocate_bits(const double* x, const double* share, int32_t n,
  * drafted tokens: project (moe_quant_linear), rotate and store
  * (moe_cache_append), attend (moe_tree_attention), project, add and normalize
  * (moe_block_norm), route and run the experts (above), add and normalize; and,
- * once the drafts have been checked, keep the accepted ones (moe_cache_keep).
+ * once the drafts have been checked (moe_draft_verify), keep the accepted ones
+ * (moe_cache_keep).  moe_qcache_* are the same steps over a cache in 8 bits.
  * The conventions above hold: caller's buffers, `stream`, host validation.
  * Tensors may differ in type; MOE_TYPE_* names the type of each.
  */
@@ -694,6 +695,154 @@ int moe_cache_keep(const moe_cache_t* C, const int32_t* table, int32_t max_pages
                    const int32_t* cache_len, int32_t n_seqs, const int32_t* new_off,
                    const int32_t* keep, int32_t max_keep, const int32_t* n_keep,
                    int32_t* len_out, int32_t* status, void* stream);
+
+/*
+ * moe_cache_append_norm -- moe_cache_append with a norm of each head before the
+ * rotation, in the same pass: a query head x becomes
+ *   x * rsqrt(mean_c(x^2) + eps) * w_q,
+ * a key head the same with w_k, and both then turn; all in fp32, rounded once.
+ *   w_q, w_k   device fp32 [head_dim] or NULL: queries (keys) as they are.
+ *   eps        >= 0.
+ * Everything else is as for moe_cache_append.
+ */
+int moe_cache_append_norm(const moe_cache_t* C, const int32_t* table, int32_t max_pages,
+                          const int32_t* cache_len, int32_t n_seqs, const int32_t* new_off,
+                          int32_t n_tokens, int32_t max_new,
+                          const void* q, int64_t ld_q, int32_t n_q_heads,
+                          const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                          const float* w_q, const float* w_k, float eps,
+                          const int32_t* positions, const float* cos, const float* sin,
+                          int32_t rot_dim, int32_t max_pos, int32_t interleaved,
+                          void* q_out, int64_t ld_q_out, int32_t* status, void* stream);
+
+/*
+ * One layer's paged key/value cache in 8 bits: half the memory, and half of what
+ * attention reads, of moe_cache_t.  Pages, tables and batches are as there.
+ *
+ * A key or value of one token and head is head_dim codes q in [-127, 127] (int8) and
+ * one scale s (fp32) and stands for s * q:
+ *   s = max_c |x_c| / 127, held between 2^-64 and 2^64,   q_c = rint(x_c / s)
+ * (a quotient within 2^-16 of half-way may round either way; a row whose values all lie
+ * below 2^-65 is zeros, and of one beyond 127 * 2^64 the large values are cut).  A row with
+ * an infinity or NaN has a NaN scale: it stands for NaN, and reaches only those who see it.
+ * Slot o of page p holds, for head g, key codes at
+ * k[((p*n_heads + g)*page_size + o)*head_dim + c], value codes, transposed inside the
+ * page, at v[((p*n_heads + g)*head_dim + c)*page_size + o], and the scales at
+ * k_scale, v_scale[(p*n_heads + g)*page_size + o].  Slots that no token has been written
+ * to may hold anything.
+ */
+typedef struct moe_qcache {
+  void*   k;            /* device int8, 16-byte aligned */
+  void*   v;            /* device int8, 16-byte aligned */
+  float*  k_scale;      /* device, 16-byte aligned */
+  float*  v_scale;      /* device, 16-byte aligned */
+  int32_t n_pages;
+  int32_t n_heads;      /* key/value heads */
+  int32_t head_dim;     /* 64, 128 or 256 */
+  int32_t page_size;    /* a power of two, 64 to 1024 */
+  int32_t type;         /* of queries, keys, values and outputs: MOE_TYPE_BF16 or MOE_TYPE_FP16 */
+  int32_t reserved0;
+} moe_qcache_t;
+
+/*
+ * moe_qcache_append -- moe_cache_append_norm into a cache in 8 bits: keys are quantized
+ * after norm and rotation, from their fp32 values, values as they come.  q_out is of C->type.
+ */
+int moe_qcache_append(const moe_qcache_t* C, const int32_t* table, int32_t max_pages,
+                      const int32_t* cache_len, int32_t n_seqs, const int32_t* new_off,
+                      int32_t n_tokens, int32_t max_new,
+                      const void* q, int64_t ld_q, int32_t n_q_heads,
+                      const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                      const float* w_q, const float* w_k, float eps,
+                      const int32_t* positions, const float* cos, const float* sin,
+                      int32_t rot_dim, int32_t max_pos, int32_t interleaved,
+                      void* q_out, int64_t ld_q_out, int32_t* status, void* stream);
+
+/*
+ * moe_qcache_read -- the keys and values that rows of a cache in 8 bits stand for, s * q
+ * rounded once to C->type: row row_off[b] + i of the outputs is token first[b] + i of sequence b,
+ * i < row_off[b+1] - row_off[b] <= max_rows (first: device int32 [n_seqs]; row_off: device
+ * int32 [n_seqs + 1], ascending, at most n_rows).  A row whose page is out of range stays as
+ * it was (MOE_ERR_SLOT in status).
+ *   k_out, v_out   device [n_rows][ld], heads side by side; either may be NULL.  Their rows
+ *                  overlap neither each other nor the cache (MOE_ERR_ARG).
+ */
+int moe_qcache_read(const moe_qcache_t* C, const int32_t* table, int32_t max_pages,
+                    const int32_t* first, int32_t n_seqs, const int32_t* row_off,
+                    int32_t n_rows, int32_t max_rows,
+                    void* k_out, int64_t ld_k_out, void* v_out, int64_t ld_v_out,
+                    int32_t* status, void* stream);
+
+/*
+ * moe_qcache_attention, moe_qcache_attention_plan -- moe_tree_attention over a cache in
+ * 8 bits, with the same arguments and meaning.  The codes enter both products as they are,
+ * exact in the 16-bit operand types; a key's scale multiplies its fp32 scores, a value's
+ * scale its softmax weight, which then is rounded to fp16 (and counts as rounded in the
+ * weights' sum; below 2^-32 of the largest product of weight and scale that the row sees
+ * it may count as zero).  Results are bitwise reproducible.
+ */
+int moe_qcache_attention_plan(const moe_qcache_t* C, int32_t n_q_heads, int32_t n_seqs,
+                              int32_t max_new, int32_t max_len, int32_t* n_split, size_t* ws_bytes);
+int moe_qcache_attention(const moe_qcache_t* C, const int32_t* table, int32_t max_pages,
+                         const int32_t* cache_len, int32_t n_seqs, const int32_t* new_off,
+                         int32_t n_tokens, int32_t max_new, int32_t max_len,
+                         const void* q, int64_t ld_q, int32_t n_q_heads,
+                         const uint64_t* mask, int32_t mask_words, float scale,
+                         void* out, int64_t ld_out, int32_t* status,
+                         void* ws, size_t ws_bytes, void* stream);
+
+/* moe_qcache_keep -- moe_cache_keep for a cache in 8 bits: codes and scales move as they are. */
+int moe_qcache_keep(const moe_qcache_t* C, const int32_t* table, int32_t max_pages,
+                    const int32_t* cache_len, int32_t n_seqs, const int32_t* new_off,
+                    const int32_t* keep, int32_t max_keep, const int32_t* n_keep,
+                    int32_t* len_out, int32_t* status, void* stream);
+
+/*
+ * moe_draft_verify -- which drafts of a batch the model accepts, and the token after them,
+ * from given random numbers: the accepted tokens and the next one are distributed as if
+ * each had been drawn from the model's own distribution.
+ *
+ * The batch is that of the cache calls: rows new_off[b] .. new_off[b+1] - 1 are sequence b's
+ * new tokens, row 0 of them its last known token, the others drafts.  With
+ * p_i = softmax(logits[i] / temperature[b]) at row i, d_i the distribution that the drafts
+ * below row i were drawn from independently (row i of `draft`), and a uniform number u of
+ * each draft:
+ *   cur = 0, r = p_0;   for the drafts i = 1, 2, ... whose parent is cur, x = tokens[i]:
+ *     u_i d_cur(x) < r(x):  accepted: cur = i, r = p_i
+ *     otherwise:            r = max(r - d_cur, 0) / its sum (r stays where that sum is 0)
+ *   next = the smallest token whose cumulated r passes u_next[b]
+ * Without `draft`, d is 1 at x (a draft that was picked, not drawn) and a refused x leaves r.
+ * Greedy (u and u_next NULL, or a sequence whose temperature is 0): a draft is accepted when
+ * it is the first of the largest logits, and next is the first of the largest.
+ *
+ *   logits       device [n_tokens][ld_logits] of logits_type (MOE_TYPE_*), `vocab` of each row; -inf: probability 0.
+ *   tokens       device int32 [n_tokens]: row's token (row 0's is not read).
+ *   parents      device int32 [n_tokens] or NULL: a draft's parent, as its index in the sequence,
+ *                below its own; -1: not below row 0, never accepted.  NULL: chains.
+ *   draft        device [n_tokens][ld_draft] of draft_type, or NULL: probabilities >= 0.
+ *   temperature  device fp32 [n_seqs] or NULL: 1.  >= 0 and finite.
+ *   u, u_next    device fp32 [n_tokens] and [n_seqs] in [0, 1), or both NULL.
+ *   keep         device int32 [n_seqs][max_new]: 0 and the accepted drafts, as moe_cache_keep
+ *                takes them, then -1.      n_keep  device int32 [n_seqs]: how many.
+ *   next         device int32 [n_seqs].
+ *                The three overlap neither each other nor an input (MOE_ERR_ARG).
+ *   ws           device workspace of moe_draft_verify_plan's bytes, 16-byte aligned.
+ * A row whose logits hold NaN or +infinity, or nothing but -infinity, has no distribution, nor
+ * has one a sequence whose temperature is negative or not finite: the walk ends there, next is
+ * -1, and MOE_ERR_RANGE is set in status.  A token or parent out of range is not accepted, and a sequence
+ * whose rows are out of range gets n_keep 0 and next -1 (MOE_ERR_SLOT).  A sequence without new
+ * tokens gets n_keep 0 and next -1.  max_new at most 1024.
+ * The last row's probabilities and sums are taken in 64 bits, those of the tests from
+ * fp32 exponentials summed in 64.  Results are bitwise reproducible.
+ */
+int moe_draft_verify_plan(int32_t n_seqs, int32_t n_tokens, int32_t max_new, int32_t vocab, size_t* ws_bytes);
+int moe_draft_verify(const void* logits, int32_t logits_type, int64_t ld_logits, int32_t n_tokens,
+                     int32_t vocab, const int32_t* tokens, const int32_t* parents,
+                     const int32_t* new_off, int32_t n_seqs, int32_t max_new,
+                     const void* draft, int32_t draft_type, int64_t ld_draft,
+                     const float* temperature, const float* u, const float* u_next,
+                     int32_t* keep, int32_t* n_keep, int32_t* next, int32_t* status,
+                     void* ws, size_t ws_bytes, void* stream);
 
 /* Human-readable name of a status code. */
 const char* moe_status_str(int status);

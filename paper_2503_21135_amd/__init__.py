@@ -14,6 +14,7 @@ from .api import (moe_code_row_words, moe_expert_ffn_mixed, moe_expert_ffn_mixed
                   moe_ffn_plan, moe_quant_pack, moe_route_permute, moe_route_workspace_bytes, moe_set_channel_switch,
                   moe_unpermute_combine,
                   moe_block_norm, moe_cache_append, moe_cache_keep, moe_quant_linear, moe_tree_attention,
-                  moe_tree_attention_plan)
-from .block import DecoderBlock, PagedCache, QuantLinear, tree_mask  # noqa: F401
+                  moe_tree_attention_plan, moe_cache_append_norm, moe_qcache_append, moe_qcache_attention,
+                  moe_qcache_attention_plan, moe_qcache_keep, moe_qcache_read, moe_draft_verify, moe_draft_verify_plan)
+from .block import DecoderBlock, DraftVerifier, PagedCache, QuantLinear, QuantPagedCache, tree_mask  # noqa: F401
 from .layer import MoELayer  # noqa: F401

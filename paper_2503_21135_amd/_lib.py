@@ -28,6 +28,8 @@ EXPORTS = (
     "moe_expert_significance", "moe_allocate_bits",
     "moe_quant_linear", "moe_block_norm",
     "moe_cache_append", "moe_cache_keep", "moe_tree_attention", "moe_tree_attention_plan",
+    "moe_cache_append_norm", "moe_qcache_append", "moe_qcache_read", "moe_qcache_attention",
+    "moe_qcache_attention_plan", "moe_qcache_keep", "moe_draft_verify", "moe_draft_verify_plan",
 )
 
 
@@ -58,6 +60,14 @@ class CacheDesc(C.Structure):
     ]
 
 
+class QuantCacheDesc(C.Structure):
+    _fields_ = [
+        ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+        ("n_pages", C.c_int32), ("n_heads", C.c_int32), ("head_dim", C.c_int32), ("page_size", C.c_int32),
+        ("type", C.c_int32), ("reserved0", C.c_int32),
+    ]
+
+
 class MoEError(RuntimeError):
     pass
 
@@ -76,6 +86,10 @@ def load() -> C.CDLL:
     L = C.CDLL(LIB_PATH)
     vp, i32, i64, sz_t, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t, C.c_float
     cache, batch = C.POINTER(CacheDesc), [vp, i32, vp, i32, vp]   # table, max_pages, cache_len, n_seqs, new_off
+    qcache = C.POINTER(QuantCacheDesc)
+    normed = batch + [i32, i32, vp, i64, i32, vp, i64, vp, i64, vp, vp, f32, vp, vp, vp, i32, i32, i32, vp, i64, vp, vp]
+    plan, keep = [i32, i32, i32, i32, C.POINTER(i32), C.POINTER(sz_t)], batch + [vp, i32, vp, vp, vp, vp]
+    attend = batch + [i32, i32, i32, vp, i64, i32, vp, i32, f32, vp, i64, vp, vp, sz_t, vp]
     sig = {
         "moe_quant_pack": (C.c_int, [vp, i64, i32, i32, i32, i32, vp, i32, vp, i64, vp, i64, i64, vp, vp]),
         "moe_route_permute": (C.c_int, [vp, i32, i32, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp,
@@ -102,10 +116,18 @@ def load() -> C.CDLL:
                                      vp, f32, vp, i64, vp, i32, i64, vp]),
         "moe_cache_append": (C.c_int, [cache] + batch + [i32, i32, vp, i64, i32, vp, i64, vp, i64, vp, vp, vp,
                                                          i32, i32, i32, vp, i64, vp, vp]),
-        "moe_tree_attention_plan": (C.c_int, [cache, i32, i32, i32, i32, C.POINTER(i32), C.POINTER(sz_t)]),
-        "moe_tree_attention": (C.c_int, [cache] + batch + [i32, i32, i32, vp, i64, i32, vp, i32, f32, vp, i64,
-                                                           vp, vp, sz_t, vp]),
-        "moe_cache_keep": (C.c_int, [cache] + batch + [vp, i32, vp, vp, vp, vp]),
+        "moe_tree_attention_plan": (C.c_int, [cache] + plan),
+        "moe_tree_attention": (C.c_int, [cache] + attend),
+        "moe_cache_keep": (C.c_int, [cache] + keep),
+        "moe_cache_append_norm": (C.c_int, [cache] + normed),
+        "moe_qcache_append": (C.c_int, [qcache] + normed),
+        "moe_qcache_read": (C.c_int, [qcache] + batch + [i32, i32, vp, i64, vp, i64, vp, vp]),
+        "moe_qcache_attention_plan": (C.c_int, [qcache] + plan),
+        "moe_qcache_attention": (C.c_int, [qcache] + attend),
+        "moe_qcache_keep": (C.c_int, [qcache] + keep),
+        "moe_draft_verify_plan": (C.c_int, [i32, i32, i32, i32, C.POINTER(sz_t)]),
+        "moe_draft_verify": (C.c_int, [vp, i32, i64, i32, i32, vp, vp, vp, i32, i32, vp, i32, i64, vp, vp, vp,
+                                       vp, vp, vp, vp, vp, sz_t, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)

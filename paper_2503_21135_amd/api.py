@@ -14,7 +14,8 @@ from typing import Optional, Tuple
 import numpy as np
 import torch
 
-from ._lib import TYPE_BF16, TYPE_FP16, TYPE_FP32, CacheDesc, LayerDesc, MoEError, check, load, stream_capturing
+from ._lib import (TYPE_BF16, TYPE_FP16, TYPE_FP32, CacheDesc, LayerDesc, MoEError, QuantCacheDesc, check, load,
+                   stream_capturing)
 
 
 def _p(t: Optional[torch.Tensor]):
@@ -387,6 +388,161 @@ def moe_cache_keep(desc: CacheDesc, table: torch.Tensor, lens: torch.Tensor, new
         _flat(status, (1,), torch.int32, "status"), _stream(stream, lens))
     if st:
         check(st, "moe_cache_keep")
+
+
+# ---------------------------------------------------------------------------
+# normed heads, the cache in 8 bits, verification of drafts
+# ---------------------------------------------------------------------------
+def _run(name: str, at: torch.Tensor, others, *args) -> None:
+    """Calls an entry point with the device of `at` current; the other tensors are on it too."""
+    dev = at.get_device()
+    for t in others:
+        if t is not None and t.get_device() != dev:
+            raise MoEError("%s: tensors on several devices" % name)
+    if dev == torch.cuda.current_device():
+        st = getattr(load(), name)(*args)
+    else:
+        with torch.cuda.device(dev):
+            st = getattr(load(), name)(*args)
+    if st:
+        check(st, name)
+
+
+def _append(name, desc, table, lens, new_off, max_new, q, k, v, q_out, w_q, w_k, eps, positions, cos, sin, interleaved,
+            status, stream) -> None:
+    N, dt, D, Hkv = k.shape[0], _DTYPE16[desc.type], desc.head_dim, desc.n_heads
+    if (q is None) != (q_out is None) or (cos is None) != (sin is None):
+        raise MoEError("q and q_out, cos and sin come in pairs")
+    tab = (1, 0) if cos is None else tuple(cos.shape)
+    qp, ld_q, Hq, op, ld_o = None, 0, 0, None, 0
+    if q is not None:
+        Hq = q.shape[1]
+        qp, ld_q = _heads(q, N, Hq, D, dt, "q")
+        op, ld_o = _heads(q_out, N, Hq, D, dt, "q_out")
+    kp, ld_k = _heads(k, N, Hkv, D, dt, "k")
+    vp, ld_v = _heads(v, N, Hkv, D, dt, "v")
+    _run(name, k, (table, lens, new_off, q, v, q_out, w_q, w_k, positions, cos, sin, status),
+         C.byref(desc), *_batch(table, lens, new_off), N, max_new, qp, ld_q, Hq, kp, ld_k, vp, ld_v,
+         _flat(w_q, (D,), torch.float32, "w_q"), _flat(w_k, (D,), torch.float32, "w_k"), eps,
+         _flat(positions, (N,), torch.int32, "positions"), _flat(cos, tab, torch.float32, "cos"),
+         _flat(sin, tab, torch.float32, "sin"), 2 * tab[1], tab[0], int(interleaved), op, ld_o,
+         _flat(status, (1,), torch.int32, "status"), _stream(stream, k))
+
+
+def moe_cache_append_norm(desc: CacheDesc, table: torch.Tensor, lens: torch.Tensor, new_off: torch.Tensor,
+                          max_new: int, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
+                          q_out: Optional[torch.Tensor], w_q: Optional[torch.Tensor], w_k: Optional[torch.Tensor],
+                          eps: float = 1e-6, positions: Optional[torch.Tensor] = None,
+                          cos: Optional[torch.Tensor] = None, sin: Optional[torch.Tensor] = None,
+                          interleaved: bool = False, status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """moe_cache_append with a norm of each head (weights w_q, w_k float32 [head_dim], None:
+    none) before the rotation."""
+    _append("moe_cache_append_norm", desc, table, lens, new_off, max_new, q, k, v, q_out, w_q, w_k, eps, positions, cos,
+            sin, interleaved, status, stream)
+
+
+def moe_qcache_append(desc: QuantCacheDesc, table: torch.Tensor, lens: torch.Tensor, new_off: torch.Tensor,
+                      max_new: int, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
+                      q_out: Optional[torch.Tensor], w_q: Optional[torch.Tensor] = None,
+                      w_k: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                      positions: Optional[torch.Tensor] = None, cos: Optional[torch.Tensor] = None,
+                      sin: Optional[torch.Tensor] = None, interleaved: bool = False,
+                      status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """moe_cache_append_norm into a cache in 8 bits."""
+    _append("moe_qcache_append", desc, table, lens, new_off, max_new, q, k, v, q_out, w_q, w_k, eps, positions, cos, sin,
+            interleaved, status, stream)
+
+
+def moe_qcache_read(desc: QuantCacheDesc, table: torch.Tensor, first: torch.Tensor, row_off: torch.Tensor, max_rows: int,
+                    k_out: Optional[torch.Tensor], v_out: Optional[torch.Tensor],
+                    status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The keys and values [rows][heads][head_dim] that rows of a cache in 8 bits stand for: row
+    row_off[b] + i is token first[b] + i of sequence b."""
+    at = k_out if k_out is not None else v_out
+    if at is None:
+        raise MoEError("k_out or v_out must be given")
+    N, dt, D, H = at.shape[0], _DTYPE16[desc.type], desc.head_dim, desc.n_heads
+    kp, ld_k = (None, 0) if k_out is None else _heads(k_out, N, H, D, dt, "k_out")
+    vp, ld_v = (None, 0) if v_out is None else _heads(v_out, N, H, D, dt, "v_out")
+    _run("moe_qcache_read", at, (table, first, row_off, v_out, status), C.byref(desc), *_batch(table, first, row_off), N,
+         max_rows, kp, ld_k, vp, ld_v, _flat(status, (1,), torch.int32, "status"), _stream(stream, at))
+
+
+def moe_qcache_attention_plan(desc: QuantCacheDesc, n_q_heads: int, n_seqs: int, max_new: int,
+                              max_len: int) -> Tuple[int, int]:
+    """(parts the keys are split into, workspace bytes) of moe_qcache_attention."""
+    ns, wb = C.c_int32(0), C.c_size_t(0)
+    check(load().moe_qcache_attention_plan(C.byref(desc), n_q_heads, n_seqs, max_new, max_len, C.byref(ns),
+                                           C.byref(wb)), "moe_qcache_attention_plan")
+    return int(ns.value), int(wb.value)
+
+
+def moe_qcache_attention(desc: QuantCacheDesc, table: torch.Tensor, lens: torch.Tensor, new_off: torch.Tensor,
+                         max_new: int, max_len: int, q: torch.Tensor, out: torch.Tensor, scale: float,
+                         mask: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                         status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """moe_tree_attention over a cache in 8 bits."""
+    N, Hq, D = q.shape
+    if D != desc.head_dim:
+        raise MoEError("q has heads of %d, the cache of %d" % (D, desc.head_dim))
+    dt = _DTYPE16[desc.type]
+    words = 0 if mask is None else mask.shape[-1]
+    qp, ld_q = _heads(q, N, Hq, D, dt, "q")
+    op, ld_o = _heads(out, N, Hq, D, dt, "out")
+    wp, wb = None, 0
+    if ws is not None:
+        if not ws.is_cuda or not ws.is_contiguous():
+            raise MoEError("ws must be a contiguous device tensor")
+        wp, wb = ws.data_ptr(), ws.numel() * ws.element_size()
+    _run("moe_qcache_attention", q, (table, lens, new_off, out, mask, ws, status),
+         C.byref(desc), *_batch(table, lens, new_off), N, max_new, max_len, qp, ld_q, Hq,
+         _flat(mask, (N, words), torch.int64, "mask"), words, scale, op, ld_o,
+         _flat(status, (1,), torch.int32, "status"), wp, wb, _stream(stream, q))
+
+
+def moe_qcache_keep(desc: QuantCacheDesc, table: torch.Tensor, lens: torch.Tensor, new_off: torch.Tensor,
+                    keep: torch.Tensor, n_keep: torch.Tensor, len_out: Optional[torch.Tensor] = None,
+                    status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """moe_cache_keep for a cache in 8 bits."""
+    B = lens.shape[0]
+    _run("moe_qcache_keep", lens, (table, new_off, keep, n_keep, len_out, status),
+         C.byref(desc), *_batch(table, lens, new_off), _flat(keep, (B, keep.shape[-1]), torch.int32, "keep"),
+         keep.shape[-1], _flat(n_keep, (B,), torch.int32, "n_keep"), _flat(len_out, (B,), torch.int32, "len_out"),
+         _flat(status, (1,), torch.int32, "status"), _stream(stream, lens))
+
+
+def moe_draft_verify_plan(n_seqs: int, n_tokens: int, max_new: int, vocab: int) -> int:
+    """Workspace bytes of moe_draft_verify."""
+    wb = C.c_size_t(0)
+    check(load().moe_draft_verify_plan(n_seqs, n_tokens, max_new, vocab, C.byref(wb)), "moe_draft_verify_plan")
+    return int(wb.value)
+
+
+def moe_draft_verify(logits: torch.Tensor, tokens: torch.Tensor, new_off: torch.Tensor, max_new: int,
+                     keep: torch.Tensor, n_keep: torch.Tensor, next_token: torch.Tensor, ws: torch.Tensor,
+                     parents: Optional[torch.Tensor] = None, draft_probs: Optional[torch.Tensor] = None,
+                     u: Optional[torch.Tensor] = None, u_next: Optional[torch.Tensor] = None,
+                     temperature: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                     stream=None) -> None:
+    """Which of the drafts tokens [tokens] the logits [tokens][vocab] accept, and the token after
+    them: keep [sequences][max_new], n_keep and next_token [sequences], all int32."""
+    N, V = logits.shape
+    B = n_keep.shape[0]
+    lp, ld = _rows(logits, N, V, "logits")
+    dp, ld_d, d_type = None, 0, 0
+    if draft_probs is not None:
+        (dp, ld_d), d_type = _rows(draft_probs, N, V, "draft_probs"), _type(draft_probs, "draft_probs")
+    i32, f32 = torch.int32, torch.float32
+    if not ws.is_cuda or not ws.is_contiguous():
+        raise MoEError("ws must be a contiguous device tensor")
+    _run("moe_draft_verify", logits, (tokens, new_off, keep, n_keep, next_token, ws, parents, draft_probs, u, u_next,
+                                      temperature, status),
+         lp, _type(logits, "logits"), ld, N, V, _flat(tokens, (N,), i32, "tokens"), _flat(parents, (N,), i32, "parents"),
+         _flat(new_off, (B + 1,), i32, "new_off"), B, max_new, dp, d_type, ld_d,
+         _flat(temperature, (B,), f32, "temperature"), _flat(u, (N,), f32, "u"), _flat(u_next, (B,), f32, "u_next"),
+         _flat(keep, (B, max_new), i32, "keep"), _flat(n_keep, (B,), i32, "n_keep"),
+         _flat(next_token, (B,), i32, "next_token"), _flat(status, (1,), i32, "status"),
+         ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream, logits))
 
 
 # ---------------------------------------------------------------------------

@@ -1,10 +1,12 @@
 """The decoder block around the expert FFN, for decoding with drafted tokens.
 
-QuantLinear   a 4-bit weight matrix in device memory and its product
-PagedCache    one layer's paged key/value cache and the calls over it
-DecoderBlock  norm -> q/k/v -> rotate and store -> attend -> project -> add and
-              norm -> MoELayer -> add and norm of the next block, one C call a step
-tree_mask     the mask words of a tree of drafts from its parents
+QuantLinear      a 4-bit weight matrix in device memory and its product
+PagedCache       one layer's paged key/value cache and the calls over it
+QuantPagedCache  the same in 8 bits
+DecoderBlock     norm -> q/k/v -> (norm,) rotate and store -> attend -> project -> add and
+                 norm -> MoELayer -> add and norm of the next block, one C call a step
+DraftVerifier    which drafts the logits accept, and the token after them
+tree_mask        the mask words of a tree of drafts from its parents
 
 The classes own buffers and marshal; every step runs in the library's kernels.
 """
@@ -17,7 +19,7 @@ import numpy as np
 import torch
 
 from . import api
-from ._lib import TYPE_BF16, TYPE_FP16, CacheDesc, MoEError
+from ._lib import TYPE_BF16, TYPE_FP16, CacheDesc, MoEError, QuantCacheDesc
 
 _TYPE16 = {torch.bfloat16: TYPE_BF16, torch.float16: TYPE_FP16}
 
@@ -67,6 +69,28 @@ class QuantLinear:
         return out
 
 
+class _Workspaces:
+    """Scratch memory per stream, which grows with the calls (it at least doubles).  A call that is
+    being captured works in memory of its graph's own pool instead: the stream of a capture is
+    not the one of its replays."""
+
+    def __init__(self, device: torch.device):
+        self.device = device
+        self._by_stream: Dict[int, torch.Tensor] = {}
+
+    def get(self, need: int, at: torch.Tensor, stream) -> Optional[torch.Tensor]:
+        if need == 0:
+            return None
+        if api._capturing(stream):
+            return api._empty((need,), torch.uint8, self.device, stream)
+        handle = api._stream(stream, at)
+        ws = self._by_stream.get(handle)
+        if ws is None or ws.numel() < need:
+            need = need if ws is None else max(need, 2 * ws.numel())
+            ws = self._by_stream[handle] = api._empty((need,), torch.uint8, self.device, stream)
+        return ws
+
+
 class PagedCache:
     """One layer's key/value cache over the caller's tensors.
 
@@ -96,7 +120,7 @@ class PagedCache:
         d.k, d.v = k.data_ptr(), v.data_ptr()
         d.n_pages, d.n_heads, d.page_size, d.head_dim, d.type = n_pages, heads, page, D, _TYPE16[k.dtype]
         self.desc = d
-        self._ws: Dict[int, torch.Tensor] = {}
+        self._ws = _Workspaces(k.device)
         self._need: Dict[tuple, int] = {}
 
     @classmethod
@@ -117,13 +141,32 @@ class PagedCache:
     def append(self, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, new_off: torch.Tensor,
                max_new: int, positions: Optional[torch.Tensor] = None, cos: Optional[torch.Tensor] = None,
                sin: Optional[torch.Tensor] = None, interleaved: bool = False,
-               q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
-        """Rotate q and k, store k and v of the new tokens; returns the rotated q."""
+               q_out: Optional[torch.Tensor] = None, stream=None, w_q: Optional[torch.Tensor] = None,
+               w_k: Optional[torch.Tensor] = None, eps: float = 1e-6) -> Optional[torch.Tensor]:
+        """Rotate q and k, store k and v of the new tokens; returns the rotated q.  w_q, w_k
+        (float32 [head_dim]): each head of q (k) is normed with them first."""
         if q is not None and q_out is None:
             q_out = api._empty(q.shape, q.dtype, q.device, stream)
-        api.moe_cache_append(self.desc, self.table, self.lens, new_off, max_new, q, k, v, q_out, positions, cos,
-                             sin, interleaved, self.status, stream)
+        self._append(new_off, max_new, q, k, v, q_out, w_q, w_k, eps, positions, cos, sin, interleaved, stream)
         return q_out
+
+    def _append(self, new_off, max_new, q, k, v, q_out, w_q, w_k, eps, positions, cos, sin, interleaved, stream) -> None:
+        if w_q is None and w_k is None:
+            api.moe_cache_append(self.desc, self.table, self.lens, new_off, max_new, q, k, v, q_out, positions, cos,
+                                 sin, interleaved, self.status, stream)
+        else:
+            api.moe_cache_append_norm(self.desc, self.table, self.lens, new_off, max_new, q, k, v, q_out, w_q, w_k, eps,
+                                      positions, cos, sin, interleaved, self.status, stream)
+
+    # the entry points of this kind of cache
+    def _plan(self, *sizes) -> int:
+        return api.moe_tree_attention_plan(self.desc, *sizes)[1]
+
+    def _attend(self, *args) -> None:
+        api.moe_tree_attention(*args)
+
+    def _keep(self, *args) -> None:
+        api.moe_cache_keep(*args)
 
     def _workspace(self, n_q_heads: int, max_new: int, max_len: int, stream) -> Optional[torch.Tensor]:
         key = (n_q_heads, self.lens.shape[0], max_new, max_len)
@@ -131,17 +174,8 @@ class PagedCache:
         if need is None:
             if len(self._need) > 4096:
                 self._need.clear()
-            need = self._need[key] = api.moe_tree_attention_plan(self.desc, *key)[1]
-        if need == 0:
-            return None
-        if api._capturing(stream):   # the stream of a capture is not the one of its replays
-            return api._empty((need,), torch.uint8, self.k.device, stream)
-        handle = api._stream(stream, self.k)
-        ws = self._ws.get(handle)
-        if ws is None or ws.numel() < need:
-            need = need if ws is None else max(need, 2 * ws.numel())
-            ws = self._ws[handle] = api._empty((need,), torch.uint8, self.k.device, stream)
-        return ws
+            need = self._need[key] = self._plan(*key)
+        return self._ws.get(need, self.k, stream)
 
     def attend(self, q: torch.Tensor, new_off: torch.Tensor, max_new: int, max_len: int,
                mask: Optional[torch.Tensor] = None, scale: Optional[float] = None,
@@ -151,9 +185,9 @@ class PagedCache:
         split).  scale: head_dim ** -0.5 unless given."""
         if out is None:
             out = api._empty(q.shape, q.dtype, q.device, stream)
-        api.moe_tree_attention(self.desc, self.table, self.lens, new_off, max_new, max_len, q, out,
-                               q.shape[2] ** -0.5 if scale is None else scale, mask,
-                               self._workspace(q.shape[1], max_new, max_len, stream), self.status, stream)
+        self._attend(self.desc, self.table, self.lens, new_off, max_new, max_len, q, out,
+                     q.shape[2] ** -0.5 if scale is None else scale, mask,
+                     self._workspace(q.shape[1], max_new, max_len, stream), self.status, stream)
         return out
 
     def keep(self, new_off: torch.Tensor, keep: torch.Tensor, n_keep: torch.Tensor,
@@ -163,8 +197,122 @@ class PagedCache:
         last layer's cache has been kept."""
         if len_out is None:
             len_out = api._empty(self.lens.shape, self.lens.dtype, self.lens.device, stream)
-        api.moe_cache_keep(self.desc, self.table, self.lens, new_off, keep, n_keep, len_out, self.status, stream)
+        self._keep(self.desc, self.table, self.lens, new_off, keep, n_keep, len_out, self.status, stream)
         return len_out
+
+
+class QuantPagedCache(PagedCache):
+    """One layer's key/value cache in 8 bits, over the caller's tensors: what PagedCache is, with
+    half the memory and half of what attention reads.
+
+    k      int8 [pages][heads][page_size][head_dim], v int8 [pages][heads][head_dim][page_size]
+    k_scale, v_scale  float32 [pages][heads][page_size]: a row stands for scale * codes
+    dtype  of queries, keys, values and outputs, bfloat16 or float16
+    """
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
+                 table: torch.Tensor, lens: torch.Tensor, dtype: torch.dtype = torch.bfloat16,
+                 status: Optional[torch.Tensor] = None):
+        if k.dim() != 4 or k.dtype != torch.int8 or v.dtype != torch.int8 or dtype not in _TYPE16:
+            raise MoEError("k and v must be 4-dimensional int8 tensors, for bfloat16 or float16")
+        n_pages, heads, page, D = k.shape
+        if tuple(v.shape) != (n_pages, heads, D, page):
+            raise MoEError("v must be [pages][heads][head_dim][page_size]: %s" % ((n_pages, heads, D, page),))
+        for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            if t.dtype != torch.float32 or tuple(t.shape) != (n_pages, heads, page):
+                raise MoEError("%s must be float32 [pages][heads][page_size]: %s" % (what, (n_pages, heads, page)))
+        for t in (k, v, k_scale, v_scale):
+            if not t.is_cuda or not t.is_contiguous() or t.device != k.device:
+                raise MoEError("k, v and their scales must be contiguous tensors of one device")
+        self.k, self.v, self.k_scale, self.v_scale, self.table, self.lens = k, v, k_scale, v_scale, table, lens
+        self.dtype = dtype
+        self.status = torch.zeros(1, dtype=torch.int32, device=k.device) if status is None else status
+        d = QuantCacheDesc()
+        d.k, d.v, d.k_scale, d.v_scale = k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr()
+        d.n_pages, d.n_heads, d.page_size, d.head_dim, d.type = n_pages, heads, page, D, _TYPE16[dtype]
+        self.desc = d
+        self._ws = _Workspaces(k.device)
+        self._need: Dict[tuple, int] = {}
+
+    @classmethod
+    def create(cls, n_seqs: int, max_len: int, n_heads: int, head_dim: int, page_size: int = 64,
+               dtype: torch.dtype = torch.bfloat16, device="cuda") -> "QuantPagedCache":
+        """An empty cache with pages of its own for every sequence's max_len tokens."""
+        per = (max_len + page_size - 1) // page_size
+        n = n_seqs * per
+        k = torch.empty(n, n_heads, page_size, head_dim, dtype=torch.int8, device=device)
+        v = torch.empty(n, n_heads, head_dim, page_size, dtype=torch.int8, device=device)
+        ks, vs = (torch.empty(n, n_heads, page_size, device=device) for _ in "kv")
+        table = torch.arange(n, dtype=torch.int32, device=device).view(n_seqs, per)
+        return cls(k, v, ks, vs, table, torch.zeros(n_seqs, dtype=torch.int32, device=device), dtype)
+
+    def _append(self, new_off, max_new, q, k, v, q_out, w_q, w_k, eps, positions, cos, sin, interleaved, stream) -> None:
+        api.moe_qcache_append(self.desc, self.table, self.lens, new_off, max_new, q, k, v, q_out, w_q, w_k, eps,
+                              positions, cos, sin, interleaved, self.status, stream)
+
+    def _plan(self, *sizes) -> int:
+        return api.moe_qcache_attention_plan(self.desc, *sizes)[1]
+
+    def _attend(self, *args) -> None:
+        api.moe_qcache_attention(*args)
+
+    def _keep(self, *args) -> None:
+        api.moe_qcache_keep(*args)
+
+    def read(self, first: torch.Tensor, row_off: torch.Tensor, max_rows: int, k_out: Optional[torch.Tensor] = None,
+             v_out: Optional[torch.Tensor] = None, rows: Optional[int] = None, stream=None):
+        """The keys and values that cached rows stand for: row row_off[b] + i is token first[b] + i
+        of sequence b, i < row_off[b+1] - row_off[b] <= max_rows.  Into k_out, v_out [rows][heads]
+        [head_dim], one of which may be left out; with neither, into new tensors of `rows` rows
+        (the most that row_off names).  Returns (k_out, v_out)."""
+        if k_out is None and v_out is None:
+            if rows is None:
+                raise MoEError("k_out, v_out or the number of rows must be given")
+            shape = (rows, self.k.shape[1], self.k.shape[3])
+            k_out, v_out = (api._empty(shape, self.dtype, self.k.device, stream) for _ in "kv")
+        api.moe_qcache_read(self.desc, self.table, first, row_off, max_rows, k_out, v_out, self.status, stream)
+        return k_out, v_out
+
+
+class DraftVerifier:
+    """Which drafts of a batch the model accepts, and the token after them, from given random
+    numbers (or greedily); with its workspace, kept per stream as PagedCache's is."""
+
+    def __init__(self, device="cuda"):
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
+        self._ws = _Workspaces(self.status.device)
+        self._need: Dict[tuple, int] = {}
+
+    def status_value(self) -> int:
+        """0, or MOE_ERR_SLOT once a token, parent or row was out of range, MOE_ERR_RANGE once a
+        row had no distribution (NaN, +infinity, nothing but -infinity); reads it back."""
+        return int(self.status.item())
+
+    def __call__(self, logits: torch.Tensor, tokens: torch.Tensor, new_off: torch.Tensor, max_new: int,
+                 parents: Optional[torch.Tensor] = None, draft_probs: Optional[torch.Tensor] = None,
+                 u: Optional[torch.Tensor] = None, u_next: Optional[torch.Tensor] = None,
+                 temperature: Optional[torch.Tensor] = None, stream=None):
+        """logits [rows][vocab] of the new tokens, row new_off[b] the last known token of sequence b,
+        its other rows drafts: tokens int32 [rows], parents int32 [rows] (index in the sequence,
+        below the draft's own; None: chains).  draft_probs [rows][vocab]: what the drafts below each
+        row were drawn from (None: they were picked).  u float32 [rows] and u_next float32
+        [sequences] in [0, 1), or neither: greedy; temperature float32 [sequences] (None: 1; 0:
+        that sequence greedily).
+
+        Returns int32 (keep [sequences][max_new], n_keep, next_token [sequences]); keep and n_keep
+        are what PagedCache.keep takes: the known token's row and the accepted drafts'."""
+        B, key = new_off.shape[0] - 1, (new_off.shape[0], logits.shape[0], max_new, logits.shape[1])
+        need = self._need.get(key)
+        if need is None:
+            if len(self._need) > 4096:
+                self._need.clear()
+            need = self._need[key] = api.moe_draft_verify_plan(B, *key[1:])
+        out = api._empty((B * (max_new + 2),), torch.int32, logits.device, stream)
+        keep, n_keep, next_token = out[:B * max_new].view(B, max_new), out[B * max_new:-B], out[B * max_new + B:]
+        api.moe_draft_verify(logits, tokens, new_off, max_new, keep, n_keep, next_token,
+                             self._ws.get(need, logits, stream), parents, draft_probs, u, u_next, temperature,
+                             self.status, stream)
+        return keep, n_keep, next_token
 
 
 class DecoderBlock:
@@ -174,7 +322,9 @@ class DecoderBlock:
 
     wqkv fp32 [(n_q_heads + 2 n_kv_heads) head_dim][d_model], wo fp32 [d_model][n_q_heads
     head_dim]; norms: dict of fp32 [d_model] with "attn" and "ffn" (before the blocks) and,
-    where the model has them, "attn_post", "ffn_post", "attn_gate", "ffn_gate".
+    where the model has them, "attn_post", "ffn_post", "attn_gate", "ffn_gate", and "q" and "k"
+    fp32 [head_dim] (of each query and key head, before it is rotated).  The caches may be
+    PagedCaches or QuantPagedCaches.
     """
 
     def __init__(self, moe, wqkv: torch.Tensor, wo: torch.Tensor, n_q_heads: int, n_kv_heads: int, head_dim: int,
@@ -202,7 +352,8 @@ class DecoderBlock:
         N, Hq, Hkv, D = h.shape[0], self.Hq, self.Hkv, self.D
         qkv = self.wqkv(h, stream=stream).view(N, Hq + 2 * Hkv, D)
         q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
-        q = cache.append(q, k, v, new_off, max_new, positions, self.cos, self.sin, stream=stream)
+        q = cache.append(q, k, v, new_off, max_new, positions, self.cos, self.sin, stream=stream,
+                         w_q=self.norms.get("q"), w_k=self.norms.get("k"), eps=self.eps)
         o = cache.attend(q, new_off, max_new, max_len, mask, 1.0 / math.sqrt(D), stream=stream)
         return self.wo(o.view(N, Hq * D), stream=stream)
 
