@@ -78,6 +78,10 @@ __device__ __forceinline__ uint32_t seen16(const QArgs& a, int64_t t, int i, int
   return (bits << below | ((1u << below) - 1)) & 0xFFFFu;
 }
 
+// lane E's value of each 16 lanes, on all of them
+template <int E>
+__device__ __forceinline__ float from_lane(float v) { return dpp<0x150 + E>(v); }
+
 // What a wave holds of its 16 RT rows.
 template <int RT, int NV>
 struct Rows16 {
@@ -95,69 +99,75 @@ struct Rows16 {
     }
   }
 
-  // Scores of 64 keys into weights: sc[rt][kt][i] is this lane's row's product with key
-  // 16 grp + 4 kt + i; k2(kt) those keys' scales times scale2, lg and rv log2 and reciprocal of the
-  // values' scales.
+  // Scores of 64 keys into weights, in two steps for row tile rt: sc[kt][i] is this lane's row's
+  // product with key 16 grp + 4 kt + i.  scales(kt) are those keys' scales times scale2, logs(kt) and
+  // inverses(kt) log2 and reciprocal of their values' scales.
   // EDGE: slots that not everybody sees (drafts, or none at all) may be among them.
-  template <bool EDGE, class K2, class LG, class RV>
-  __device__ __forceinline__ void weigh(f32x4 (&sc)[RT][4], K2 k2, LG lg, RV rv, const uint32_t (&see)[RT], u32x4 (&pf)[RT][2]) {
+  template <bool EDGE, class S, class L>
+  __device__ __forceinline__ void exponents(int rt, f32x4 (&sc)[4], S scales, L logs, uint32_t see) {
+    float most = -INFINITY;
 #pragma unroll
     for (int kt = 0; kt < 4; kt++) {
-      const f32x4 k = k2(kt), g = lg(kt);
+      const f32x4 k2 = scales(kt), lg = logs(kt);
 #pragma unroll
-      for (int rt = 0; rt < RT; rt++)
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-          float x = __fmaf_rn(sc[rt][kt][i], k[i], g[i]);
-          if constexpr (EDGE) x = see[rt] >> (4 * kt + i) & 1 ? x : -INFINITY;
-          sc[rt][kt][i] = x;
-        }
+      for (int i = 0; i < 4; i++) {
+        float x = __fmaf_rn(sc[kt][i], k2[i], lg[i]);
+        if constexpr (EDGE) x = see >> (4 * kt + i) & 1 ? x : -INFINITY;
+        sc[kt][i] = x;
+      }
+      most = fmaxf(most, fmaxf(fmaxf(sc[kt][0], sc[kt][1]), fmaxf(sc[kt][2], sc[kt][3])));
     }
-    __builtin_amdgcn_sched_barrier(0);   // the scales' registers are free again
+    // A row's maximum moves only when an exponent passes it by kSlack: until then no lane asks
+    // the others for theirs.  (A row that has seen nothing has -infinity, which any passes.)
+    if (__any(!(most <= ms[rt] + (kSlack + kLift)))) {
+      const float all = rows_max(most);
+      const bool moves = !(all <= ms[rt] + (kSlack + kLift));    // this row, whatever its neighbours do
+      const float m2 = moves ? fmaxf(m[rt], all) : m[rt];
+      const float ms2 = m2 == -INFINITY ? 0.f : m2 - kLift;
+      const float f = m[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms[rt] - ms2);
+      l[rt] *= f;
 #pragma unroll
-    for (int rt = 0; rt < RT; rt++) {
-      float most = -INFINITY;
+      for (int v = 0; v < NV; v++)
 #pragma unroll
-      for (int kt = 0; kt < 4; kt++)
-        most = fmaxf(most, fmaxf(fmaxf(sc[rt][kt][0], sc[rt][kt][1]), fmaxf(sc[rt][kt][2], sc[rt][kt][3])));
-      // A row's maximum moves only when an exponent passes it by kSlack: until then no lane asks
-      // the others for theirs.  (A row that has seen nothing has -infinity, which any passes.)
-      if (__any(!(most <= ms[rt] + (kSlack + kLift)))) {
-        const float all = rows_max(most);
-        const bool moves = !(all <= ms[rt] + (kSlack + kLift));    // this row, whatever its neighbours do
-        const float m2 = moves ? fmaxf(m[rt], all) : m[rt];
-        const float ms2 = m2 == -INFINITY ? 0.f : m2 - kLift;
-        const float f = m[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms[rt] - ms2);
-        l[rt] *= f;
+        for (int i = 0; i < 4; i++) o[rt][v][i] *= f;
+      m[rt] = m2;
+      ms[rt] = m2 == -INFINITY ? -INFINITY : ms2;
+    }
+  }
+  template <bool EDGE, class V>
+  __device__ __forceinline__ void weights(int rt, const f32x4 (&sc)[4], V inverses, uint32_t see, u32x4 (&pf)[2]) {
+    const float by = ms[rt] == -INFINITY ? 0.f : ms[rt];
+    // Cut to fp16's bits in fp32 first: their sum takes the cut weights, so that the cut of one
+    // that outweighs the rest cancels, and still has those whose value scale is so small that
+    // the product is below fp16's range (a row of zeros takes its share of the softmax).
 #pragma unroll
-        for (int v = 0; v < NV; v++)
+    for (int kt = 0; kt < 4; kt++) {
+      const f32x4 rv = inverses(kt);
+      float p[4];
 #pragma unroll
-          for (int i = 0; i < 4; i++) o[rt][v][i] *= f;
-        m[rt] = m2;
-        ms[rt] = m2 == -INFINITY ? -INFINITY : ms2;
-      }
-      const float by = ms[rt] == -INFINITY ? 0.f : ms[rt];
-#pragma unroll
-      for (int i = 0; i < 8; i++) {
-        // Cut to fp16's bits in fp32 first: their sum takes the cut weights, so that the cut of one
-        // that outweighs the rest cancels, and still has those whose value scale is so small that
-        // the product is below fp16's range (a row of zeros takes its share of the softmax).
-        float p[2];
-        const f32x4 rv4 = rv(i / 2);
-#pragma unroll
-        for (int e = 0; e < 2; e++) {
-          const int j = 2 * i + e;
-          p[e] = __uint_as_float(__float_as_uint(__builtin_amdgcn_exp2f(sc[rt][j >> 2][j & 3] - by)) & 0xFFFFE000u);
-          if constexpr (EDGE) p[e] = see[rt] >> j & 1 ? p[e] : 0.f;
-          const float r = __fmaf_rn(p[e], rv4[j & 3], l[rt]);
-          if constexpr (EDGE) l[rt] = see[rt] >> j & 1 ? r : l[rt];
-          else l[rt] = r;
+      for (int i = 0; i < 4; i++) {
+        p[i] = __uint_as_float(__float_as_uint(__builtin_amdgcn_exp2f(sc[kt][i] - by)) & 0xFFFFE000u);
+        float r = __fmaf_rn(p[i], rv[i], l[rt]);
+        if constexpr (EDGE) {
+          p[i] = see >> (4 * kt + i) & 1 ? p[i] : 0.f;
+          r = see >> (4 * kt + i) & 1 ? r : l[rt];
         }
-        pf[rt][i >> 2][i & 3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(p[0], p[1]));
+        l[rt] = r;
       }
+      pf[kt >> 1][kt % 2 * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(p[0], p[1]));
+      pf[kt >> 1][kt % 2 * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(p[2], p[3]));
     }
   }
 };
+
+// Lane 16 grp + e's value of what belongs to keys 16 grp + (0..15), as keys 16 grp + 4 kt + (0..3) of
+// each group's lanes.
+__device__ __forceinline__ f32x4 from_lanes(float v, int kt) {
+  if (kt == 0) return f32x4{from_lane<0>(v), from_lane<1>(v), from_lane<2>(v), from_lane<3>(v)};
+  if (kt == 1) return f32x4{from_lane<4>(v), from_lane<5>(v), from_lane<6>(v), from_lane<7>(v)};
+  if (kt == 2) return f32x4{from_lane<8>(v), from_lane<9>(v), from_lane<10>(v), from_lane<11>(v)};
+  return f32x4{from_lane<12>(v), from_lane<13>(v), from_lane<14>(v), from_lane<15>(v)};
+}
 
 // Few rows, straight from memory: four waves on the same 16 RT rows, each with keys of its own.
 // Many rows (RW > 1): RW waves on 16 RT rows each by KW groups of keys; a group's waves read its
@@ -178,7 +188,7 @@ __global__ void __launch_bounds__(64 * RW * KW, RW * KW == 8 || (RW == 1 && D <=
     Tile tile[2][KW];
     Sums sums;
   };
-  constexpr bool kShared = RW > 1;
+  constexpr bool kShared = RW > 1, kAhead = RT * D <= 128;
   __shared__ __attribute__((aligned(16))) char lds_bytes[kShared ? (KW > 1 ? sizeof(Lds) : sizeof(Tile) * 2) : sizeof(Sums)];
   __shared__ float stats[W][RT][16][2];
   // row blocks of a unit (sequence, head, part) sit 8 workgroups apart, on one XCD, and
@@ -235,64 +245,90 @@ __global__ void __launch_bounds__(64 * RW * KW, RW * KW == 8 || (RW == 1 && D <=
   if constexpr (!kShared) {
     const int krow = 16 * (col >> 2) + (col & 3);
     const uint32_t k_off = krow * D + 16 * grp, v_off = col * P + 16 * grp;
-    auto step = [&](auto edge_c, int page, int t) {
-      constexpr bool EDGE = decltype(edge_c)::value;
-      const int in_page = t * kTile & (P - 1);
-      const int64_t head = head_at(page);
-      const uint8_t *kp = static_cast<const uint8_t*>(a.kc) + (head + in_page) * D, *vp = static_cast<const uint8_t*>(a.vc) + head * D + in_page;
-      u32x4 kf[4][D / 64], vf[NV];
+    auto load_k = [&](u32x4 (&kf)[4][D / 64], int page, int t) {
+      const uint8_t* p = static_cast<const uint8_t*>(a.kc) + (head_at(max(page, 0)) + (t * kTile & (P - 1))) * D;
 #pragma unroll
       for (int kt = 0; kt < 4; kt++)
 #pragma unroll
-        for (int c = 0; c < D / 64; c++) kf[kt][c] = *reinterpret_cast<const u32x4*>(kp + (k_off + 4 * kt * D + 64 * c));
-      f32x4 ks[4], vs[4];
+        for (int c = 0; c < D / 64; c++) kf[kt][c] = *reinterpret_cast<const u32x4*>(p + (k_off + 4 * kt * D + 64 * c));
+    };
+    auto load_v = [&](u32x4 (&vf)[NV], float& ks, float& vs, int page, int t) {
+      const int in_page = t * kTile & (P - 1);
+      const int64_t head = head_at(max(page, 0));
+      const uint8_t* p = static_cast<const uint8_t*>(a.vc) + head * D + in_page;
 #pragma unroll
-      for (int kt = 0; kt < 4; kt++) {
-        ks[kt] = *reinterpret_cast<const f32x4*>(a.ks + head + in_page + 16 * grp + 4 * kt);
-        vs[kt] = *reinterpret_cast<const f32x4*>(a.vs + head + in_page + 16 * grp + 4 * kt);
-      }
-#pragma unroll
-      for (int v = 0; v < NV; v++) vf[v] = *reinterpret_cast<const u32x4*>(vp + 16 * v * P + v_off);
+      for (int v = 0; v < NV; v++) vf[v] = *reinterpret_cast<const u32x4*>(p + 16 * v * P + v_off);
+      ks = a.ks[head + in_page + lane];
+      vs = a.vs[head + in_page + lane];
+    };
+    auto step = [&](auto edge_c, const u32x4 (&kf)[4][D / 64], const u32x4 (&vf)[NV], float ks, float vs, int t) {
+      constexpr bool EDGE = decltype(edge_c)::value;
       uint32_t see[RT];
       if constexpr (EDGE) see_of(see, t);
       f32x4 sc[RT][4];
 #pragma unroll
-      for (int kt = 0; kt < 4; kt++)
+      for (int kt = 0; kt < 4; kt++) {
 #pragma unroll
         for (int c = 0; c < D / 32; c++) {
-          const u32x4 k = operand<TYPE>(kf[kt][c / 2], c % 2);
+          u32x4 codes = kf[kt][c / 2];
+          asm("" : "+v"(codes));   // codes, not widened keys, are what waits for its turn in registers
+          const u32x4 k = operand<TYPE>(codes, c % 2);
 #pragma unroll
           for (int rt = 0; rt < RT; rt++) sc[rt][kt] = product<TYPE>(k, qf[rt][c], c ? sc[rt][kt] : f32x4{0.f, 0.f, 0.f, 0.f});
         }
-      __builtin_amdgcn_sched_barrier(0);
+      }
       u32x4 pf[RT][2];
-      auto each = [](const f32x4& x, auto f) { return f32x4{f(x[0]), f(x[1]), f(x[2]), f(x[3])}; };
-      st.template weigh<EDGE>(
-          sc, [&](int kt) { return ks[kt] * f32x4{a.scale2, a.scale2, a.scale2, a.scale2}; },
-          [&](int kt) { return each(vs[kt], [](float x) { return __builtin_amdgcn_logf(x); }); },
-          [&](int kt) { return each(vs[kt], [](float x) { return __builtin_amdgcn_rcpf(x); }); }, see, pf);
-      __builtin_amdgcn_sched_barrier(0);
+      const float k2 = ks * a.scale2, lg = __builtin_amdgcn_logf(vs), rv = __builtin_amdgcn_rcpf(vs);
 #pragma unroll
-      for (int v = 0; v < NV; v++) {
+      for (int rt = 0; rt < RT; rt++) {
+        st.template exponents<EDGE>(rt, sc[rt], [&](int kt) { return from_lanes(k2, kt); }, [&](int kt) { return from_lanes(lg, kt); }, see[rt]);
+        st.template weights<EDGE>(rt, sc[rt], [&](int kt) { return from_lanes(rv, kt); }, see[rt], pf[rt]);
+      }
+#pragma unroll
+      for (int v = 0; v < NV; v++)
 #pragma unroll
         for (int e = 0; e < 2; e++) {
           const u32x4 w = operand<MOE_TYPE_FP16>(vf[v], e);
 #pragma unroll
           for (int rt = 0; rt < RT; rt++) st.o[rt][v] = product<MOE_TYPE_FP16>(w, pf[rt][e], st.o[rt][v]);
         }
-        if (v % 2) __builtin_amdgcn_sched_barrier(0);
-      }
     };
+    // the next tile's keys load behind this one's products; tiles with drafts in them, the
+    // last ones, go one at a time
     int n = 0, t = t_first + wave;
-    auto run = [&](auto edge_c, int end) {
-      for (; t < end; t += W, n++) {
-        if (n % kWave == 0) look_up(n);
-        const int page = __builtin_amdgcn_readlane(pages, n % kWave);
-        if (page >= 0) step(edge_c, page, t);
-      }
+    auto next_page = [&]() {
+      if (++n % kWave == 0) look_up(n);
+      return static_cast<int>(__builtin_amdgcn_readlane(pages, n % kWave));
     };
-    run(std::false_type{}, t_full);
-    run(std::true_type{}, t_end);
+    look_up(0);
+    int page = __builtin_amdgcn_readfirstlane(pages);
+    u32x4 kf[4][D / 64], vf[NV];
+    float ks, vs;
+    if (t < t_full) {
+      u32x4 kn[4][D / 64];
+      load_k(kf, page, t);
+      for (; t < t_full; t += W) {
+        load_v(vf, ks, vs, page, t);
+        const int next = next_page();
+        if (kAhead && t + W < t_full) load_k(kn, next, t + W);
+        if (page >= 0) step(std::false_type{}, kf, vf, ks, vs, t);
+        if (!kAhead && t + W < t_full) load_k(kn, next, t + W);
+#pragma unroll
+        for (int kt = 0; kt < 4; kt++)
+#pragma unroll
+          for (int c = 0; c < D / 64; c++) kf[kt][c] = kn[kt][c];
+        page = next;
+      }
+    }
+#pragma unroll 1
+    for (; t < t_end; t += W) {
+      if (page >= 0) {
+        load_k(kf, page, t);
+        load_v(vf, ks, vs, page, t);
+        step(std::true_type{}, kf, vf, ks, vs, t);
+      }
+      page = next_page();
+    }
   } else {
     Lds& lds = *reinterpret_cast<Lds*>(lds_bytes);
     const int tid = threadIdx.x % TG;
@@ -353,6 +389,7 @@ __global__ void __launch_bounds__(64 * RW * KW, RW * KW == 8 || (RW == 1 && D <=
       uint32_t see[RT];
       if constexpr (EDGE) see_of(see, t);
       f32x4 sc[RT][4];
+      u32x4 pf[RT][2];
 #pragma unroll
       for (int kt = 0; kt < 4; kt++)
 #pragma unroll
@@ -361,11 +398,12 @@ __global__ void __launch_bounds__(64 * RW * KW, RW * KW == 8 || (RW == 1 && D <=
 #pragma unroll
           for (int rt = 0; rt < RT; rt++) sc[rt][kt] = product<TYPE>(k, qf[rt][c], c ? sc[rt][kt] : f32x4{0.f, 0.f, 0.f, 0.f});
         }
-      __builtin_amdgcn_sched_barrier(0);
-      u32x4 pf[RT][2];
-      st.template weigh<EDGE>(sc, [&](int kt) { return tile.k2[4 * grp + kt]; }, [&](int kt) { return tile.lg[4 * grp + kt]; },
-                              [&](int kt) { return tile.rv[4 * grp + kt]; }, see, pf);
-      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (D == 256) __builtin_amdgcn_sched_barrier(0);   // values read ahead would not fit
+#pragma unroll
+      for (int rt = 0; rt < RT; rt++)
+        st.template exponents<EDGE>(rt, sc[rt], [&](int kt) { return tile.k2[4 * grp + kt]; }, [&](int kt) { return tile.lg[4 * grp + kt]; }, see[rt]);
+#pragma unroll
+      for (int rt = 0; rt < RT; rt++) st.template weights<EDGE>(rt, sc[rt], [&](int kt) { return tile.rv[4 * grp + kt]; }, see[rt], pf[rt]);
 #pragma unroll
       for (int v = 0; v < NV; v++)
 #pragma unroll
@@ -468,8 +506,12 @@ __global__ void __launch_bounds__(64 * RW * KW, RW * KW == 8 || (RW == 1 && D <=
 }
 
 // How a batch is laid over workgroups.  Up to 16 rows (32 where the registers allow two tiles)
-// per key head go straight from memory, more through LDS.  Parts: enough for 1024 workgroups
-// straight from memory, 256 through LDS, and no shorter than two steps of every wave.
+// per key head go straight from memory, more through LDS, whose tiles are shared by as many waves
+// as there are row tiles.  Parts: as many as make the workgroups that are resident at once (four a
+// CU of head_dim 64 straight from memory, two of 128, one otherwise), the nearest number to it,
+// since a few too many run alone at the end (64 sequences by 8 heads of 128 over up to 4096: 84.0 us
+// in 512 workgroups, 88.5 in 1024; 30 x 4 heads of 256 over 4000 62.3 in 240, 73.2 in 360; 6 x 8
+// heads, 64 rows over 8000, 36.3 in 240, 50.8 in 288), and no shorter than two steps of every wave.
 struct Plan {
   int row_waves;   // RW of the kernel
   int row_tiles;   // 16-row tiles of a wave
@@ -489,8 +531,8 @@ Plan plan_of(const moe_qcache_t* C, int n_q_heads, int n_seqs, int max_new, int 
   const int key_waves = p.row_waves == 1 ? 4 : p.row_waves == 4 && !wide ? 2 : 1;
   p.threads = 64 * p.row_waves * key_waves;
   const int64_t wgs = std::max<int64_t>(1, static_cast<int64_t>(n_seqs) * C->n_heads * p.row_blocks);
-  const int64_t tiles = std::max<int64_t>(1, cdiv(max_len, kTile));
-  const int64_t want = std::max<int64_t>(1, std::min<int64_t>({cdiv(p.row_waves == 1 ? 1024 : 256, wgs), tiles / (2 * key_waves), kMaxSplit}));
+  const int64_t tiles = std::max<int64_t>(1, cdiv(max_len, kTile)), slots = p.row_waves == 1 ? 65536 / C->head_dim : 256;
+  const int64_t want = std::max<int64_t>(1, std::min<int64_t>({(slots + wgs / 2) / wgs, tiles / (2 * key_waves), kMaxSplit}));
   p.part_tiles = static_cast<int>(cdiv(tiles, want));
   p.n_split = static_cast<int>(cdiv(tiles, p.part_tiles));
   return p;

@@ -1,16 +1,18 @@
 // verify.hip -- moe_draft_verify: which drafted tokens a model accepts, and the token after
 // them, from given random numbers.
 //
-// Whether a draft is accepted, once the walk stands at its parent and has refused its elder
-// siblings, does not depend on the rest of the walk: so every draft is tested at once, and the
-// walk follows the answers.  Four steps:
-//   stats_kernel    per row and chunk of the vocabulary: maximum, first index of it, sum of
-//                   exponentials                                    (reads every logit once)
-//   level_kernel    trees with draft probabilities: per row the sums that remain after each
-//                   refused sibling but the last
-//   walk_kernel     per sequence: the tests, the walk, keep, and what is drawn from
-//   total_kernel    per sequence and chunk: the sum of what remains at the walk's end, 64 bits
-//   pick_kernel     per sequence: the chunk, and the token in it, that u_next falls on
+// With draft probabilities d, what is left of p after refusals is always max(p - c d, 0) over its
+// sum S(c): a refusal turns (p - c d)+ / S into ((p - c d)+ / S - d)+ = (p - (c + S) d)+ / S, so c
+// grows by S, from c = 0, S = 1.  One refusal costs one sum over a row, and its sums by chunk of
+// the vocabulary are what the next token is drawn from if the walk ends there.  Without
+// probabilities a refusal takes one token out, and nothing is summed before the end.
+//   stats_kernel   per row and chunk: maximum and sum of exponentials, or the first of the
+//                  largest                                      (reads every logit once)
+//   walk_kernel    per sequence: rows' statistics, drafts' probabilities, the walk to its end or
+//                  to the first sum that it needs
+//   pass_kernel    per sequence and chunk: that sum; the last workgroup of a sequence adds up and
+//                  walks on, and at the end of the walk draws.  Launched once for chains and picked
+//                  drafts, kPasses times for drawn trees; the last launch sees to the rest alone.
 #include <algorithm>
 
 #include "elem.hpp"
@@ -20,22 +22,36 @@ namespace verify {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kChunk = 4096;        // tokens of the vocabulary of a workgroup
+constexpr int kWaves = kThreads / kWave;
+constexpr int kChunk = 1024;        // tokens of the vocabulary of a pass's workgroup
 constexpr int kEach = kChunk / kThreads;
 constexpr int kMaxNew = 1024;
+constexpr int kPasses = 4;
+
+// Where a sequence's walk stands.
+struct State {
+  double c, s;      // what is left of row cur's p: (p - c d)+ / s
+  double sum;       // the row's sum and maximum
+  float top;
+  int cur, at;      // the row, and the last draft that was tested
+  int count;        // kept rows
+  int need;         // what a pass has to sum: nothing any more, a refusal, or what is drawn from
+};
+enum { kDone = 0, kRefusal = 1, kDraw = 2 };
 
 struct Args {
   const void *logits, *draft;
   const int32_t *tokens, *parents, *off;
   const float *temperature, *u, *u_next;
   int32_t *keep, *n_keep, *next, *status;
-  double *sum, *level, *total;   // [n_tokens][chunks], [n_tokens], [n_seqs][chunks]
-  float* top;                    // [n_tokens][chunks]
-  int32_t *arg, *end;            // [n_tokens][chunks], [n_seqs]: the walk's last row, -1: nothing to draw
-  double *row_sum;               // [n_tokens]: of each row, and its maximum
-  float *row_top;
+  double *sum, *total, *row_sum, *prob;   // [n_tokens][blocks], [n_seqs][chunks], [n_tokens], [n_tokens]
+  float *top, *row_top, *share;           // [n_tokens][blocks], [n_tokens], [n_tokens]
+  int32_t *arg, *above;                   // [n_tokens][blocks], [n_tokens]: parents, -1 where not acceptable
+  State* state;                           // [n_seqs]
+  unsigned* arrived;                      // [n_seqs]
   int64_t ld, ld_draft;
-  int n_seqs, n_tokens, max_new, vocab, chunks, type, draft_type;
+  int n_seqs, n_tokens, max_new, vocab, type, draft_type;
+  int blocks, chunks;                     // of a row: of its statistics, and of a pass
 };
 
 struct Seq { int off, n; };
@@ -50,467 +66,526 @@ __device__ __forceinline__ Seq sequence(const Args& a, int b, bool& ok) {
   return s;
 }
 __device__ __forceinline__ float heat_of(const Args& a, int b) { return a.temperature ? a.temperature[b] : 1.f; }
-__device__ __forceinline__ bool greedy(const Args& a, int b) { return !a.u || heat_of(a, b) == 0.f; }
 
-// 16 consecutive logits or probabilities from any aligned address, past the end -inf
-template <int TYPE>
-__device__ __forceinline__ void load16(const void* base, int64_t at, int left, float fill, float (&x)[kEach]) {
+// N values from `at` on, wherever they start; `fill` from `left` on
+template <int TYPE, int N>
+__device__ __forceinline__ void load_some(const void* base, int64_t at, int left, float fill, float (&x)[N]) {
   typedef elem_t<TYPE> E;
-  struct __attribute__((packed, aligned(sizeof(E)))) Piece { E e[16 / sizeof(E)]; };
-  constexpr int N = 16 / sizeof(E);
+  constexpr int M = std::min<int>(16 / sizeof(E), N);
+  struct __attribute__((packed, aligned(sizeof(E)))) Piece { E e[M]; };
   const E* p = static_cast<const E*>(base) + at;
-  if (left >= kEach) {
+  if (left >= N) {
 #pragma unroll
-    for (int i = 0; i < kEach / N; i++) {
+    for (int i = 0; i < N / M; i++) {
       const Piece w = reinterpret_cast<const Piece*>(p)[i];
 #pragma unroll
-      for (int e = 0; e < N; e++) x[i * N + e] = static_cast<float>(w.e[e]);
+      for (int e = 0; e < M; e++) x[i * M + e] = static_cast<float>(w.e[e]);
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < kEach; i++) x[i] = i < left ? static_cast<float>(p[i]) : fill;
+    for (int i = 0; i < N; i++) x[i] = i < left ? static_cast<float>(p[i]) : fill;
   }
 }
-__device__ __forceinline__ void load16(int type, const void* base, int64_t at, int left, float fill, float (&x)[kEach]) {
-  if (type == MOE_TYPE_FP32) load16<MOE_TYPE_FP32>(base, at, left, fill, x);
-  else if (type == MOE_TYPE_BF16) load16<MOE_TYPE_BF16>(base, at, left, fill, x);
-  else load16<MOE_TYPE_FP16>(base, at, left, fill, x);
+template <int N>
+__device__ __forceinline__ void load_some(int type, const void* base, int64_t at, int left, float fill, float (&x)[N]) {
+  if (type == MOE_TYPE_FP32) load_some<MOE_TYPE_FP32>(base, at, left, fill, x);
+  else if (type == MOE_TYPE_BF16) load_some<MOE_TYPE_BF16>(base, at, left, fill, x);
+  else load_some<MOE_TYPE_FP16>(base, at, left, fill, x);
 }
-
-// exp(d / heat) for d <= 0, the argument's rounding errors taken along
-struct Exp {
-  float hi, lo;   // log2(e) / heat
-  __device__ explicit Exp(float heat) {
-    const double c = fmin(1.4426950408889634 / static_cast<double>(heat), 1e30);
-    hi = static_cast<float>(c);
-    lo = static_cast<float>(c - hi);
-  }
-  __device__ float operator()(float d) const {
-    const float t = d * hi, e = __builtin_amdgcn_exp2f(t);
-    const float r = __fmaf_rn(e, (__fmaf_rn(d, hi, -t) + d * lo) * 0.69314718f, e);
-    return t < -120.f ? 0.f : r;
-  }
-};
 
 __device__ __forceinline__ double wave_sum64(double v) {
   for (int w = 32; w; w >>= 1) v += __shfl_xor(v, w);
   return v;
 }
+__device__ __forceinline__ float wave_max(float v) {
+  v = fmaxf(v, dpp<0xB1>(v));
+  v = fmaxf(v, dpp<0x4E>(v));
+  v = fmaxf(v, dpp<0x141>(v));
+  v = fmaxf(v, dpp<0x140>(v));
+  return rows_max(v);
+}
+// log2(e) / heat, finite for the smallest
+__device__ __forceinline__ float rate_of(float heat) { return fminf(1.44269504088896340736f / heat, 1e30f); }
 
+// The exponentials' arguments are products of an exact difference, and each is off by 2^-24 of
+// itself at most: a row's sum by about 10^-7 of itself, which the tests compare to.
+template <int TYPE, int EACH>
 __global__ void __launch_bounds__(kThreads) stats_kernel(Args a) {
-  __shared__ float tops[kThreads / kWave];
-  __shared__ int args[kThreads / kWave];
-  __shared__ double sums[kThreads / kWave];
-  const int chunk = blockIdx.x, i = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
+  __shared__ float tops[kWaves];
+  __shared__ double sums[kWaves];
+  __shared__ int args[kWaves];
+  const int block = blockIdx.x, i = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
   bool ok;
   const Seq s = sequence(a, b, ok);
+  const float heat = heat_of(a, b);
   if (i >= s.n) return;
+  const bool greedy = !a.u || heat == 0.f;
   const int64_t row = s.off + i;
-  const int at = chunk * kChunk + tid * kEach;
-  float x[kEach];
-  load16(a.type, a.logits, row * a.ld + at, a.vocab - at, -INFINITY, x);
-  float top = -INFINITY;
-  int arg = 0;
-  bool nan = false;
+  // 16 bytes of a lane side by side
+  constexpr int M = 16 / sizeof(elem_t<TYPE>), kPieces = EACH / M;
+  float x[kPieces][M];
+  const int at = block * (kThreads * EACH) + tid * M;
+  const bool whole = (block + 1) * static_cast<int64_t>(kThreads * EACH) <= a.vocab;   // the loads need not wait for each other
 #pragma unroll
-  for (int e = 0; e < kEach; e++) {
-    nan = nan || x[e] != x[e];
-    if (x[e] > top) {
-      top = x[e];
-      arg = at + e;
-    }
-  }
-  for (int w = 32; w; w >>= 1) {
-    const float t = __shfl_xor(top, w);
-    const int g = __shfl_xor(arg, w);
-    if (t > top || (t == top && g < arg)) {
-      top = t;
-      arg = g;
-    }
+  for (int p = 0; p < kPieces; p++)
+    load_some<TYPE>(a.logits, row * a.ld + at + p * kThreads * M, whole ? M : a.vocab - at - p * kThreads * M, -INFINITY, x[p]);
+  float top = -INFINITY;
+#pragma unroll
+  for (int p = 0; p < kPieces; p++)
+#pragma unroll
+    for (int e = 0; e < M; e++) top = fmaxf(top, x[p][e]);
+  top = wave_max(top);
+  double sum = 0.;
+  int arg = INT32_MAX;
+  if (greedy) {
+    bool nan = false;
+#pragma unroll
+    for (int p = kPieces - 1; p >= 0; p--)
+#pragma unroll
+      for (int e = M - 1; e >= 0; e--) {
+        nan = nan || x[p][e] != x[p][e];
+        if (x[p][e] == top) arg = at + p * kThreads * M + e;
+      }
+    for (int w = 32; w; w >>= 1) arg = min(arg, __shfl_xor(arg, w));
+    if (__any(nan)) sum = __builtin_nan("");
+  } else {
+    const float rate = rate_of(heat), base = top == -INFINITY ? 0.f : top;
+    float part = 0.f;
+#pragma unroll
+    for (int p = 0; p < kPieces; p++)
+#pragma unroll
+      for (int e = 0; e < M; e++) part += __builtin_amdgcn_exp2f((x[p][e] - base) * rate);
+    sum = wave_sum64(part);
   }
   if (tid % kWave == 0) {
     tops[tid / kWave] = top;
+    sums[tid / kWave] = sum;
     args[tid / kWave] = arg;
   }
   __syncthreads();
-  for (int w = 0; w < kThreads / kWave; w++)
-    if (tops[w] > top || (tops[w] == top && args[w] < arg)) {
-      top = tops[w];
-      arg = args[w];
-    }
-  double sum = 0.;
-  if (!greedy(a, b)) {
-    const Exp ex(heat_of(a, b));
-    const float base = top == -INFINITY ? 0.f : top;
-#pragma unroll
-    for (int e = 0; e < kEach; e++) sum += static_cast<double>(ex(x[e] - base));
-  }
-  if (nan) sum = __builtin_nan("");
-  sum = wave_sum64(sum);
-  if (tid % kWave == 0) sums[tid / kWave] = sum;
-  __syncthreads();
   if (tid == 0) {
-    for (int w = 1; w < kThreads / kWave; w++) sum += sums[w];
-    a.top[row * a.chunks + chunk] = top;
-    a.arg[row * a.chunks + chunk] = arg;
-    a.sum[row * a.chunks + chunk] = sum;
-  }
-}
-
-// A row's probability of a token, in 64 bits.
-__device__ __forceinline__ double prob(const Args& a, double x, float top, double sum, double heat) {
-  return exp((x - top) / heat) / sum;
-}
-
-// what remains of p after the refused siblings whose sums are in `levels`, n of them; a sum of 0
-// refused nothing
-__device__ __forceinline__ double remains(double p, double d, const double* levels, int n) {
-  double r = p, z = 1.;
-  for (int k = 0; k < n; k++) {
-    if (levels[k] == 0.) continue;
-    r = fmax(r / z - d, 0.);
-    z = levels[k];
-  }
-  return r / z;
-}
-
-// combines a row's chunks: all lanes of a wave get the maximum, its first index and the sum
-__device__ __forceinline__ void join_row(const Args& a, int64_t row, Exp ex, int lane, float& top, int& arg, double& sum) {
-  top = -INFINITY;
-  arg = 0;
-  for (int c = lane; c < a.chunks; c += kWave) {
-    const float t = a.top[row * a.chunks + c];
-    if (t > top) {
-      top = t;
-      arg = a.arg[row * a.chunks + c];
-    }
-  }
-  for (int w = 32; w; w >>= 1) {
-    const float t = __shfl_xor(top, w);
-    const int g = __shfl_xor(arg, w);
-    if (t > top || (t == top && g < arg)) {
-      top = t;
-      arg = g;
-    }
-  }
-  sum = 0.;
-  for (int c = lane; c < a.chunks; c += kWave) {
-    const float t = a.top[row * a.chunks + c];
-    sum += a.sum[row * a.chunks + c] * (t == top ? 1. : t == -INFINITY ? 1. : static_cast<double>(ex(t - top)));
-  }
-  sum = wave_sum64(sum);
-}
-
-// Per row: its own statistics, and for trees with draft probabilities the level sums.
-__global__ void __launch_bounds__(kThreads) level_kernel(Args a) {
-  __shared__ int kids[kMaxNew], n_kids;
-  __shared__ double levels[kMaxNew], parts[kThreads / kWave];
-  const int i = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
-  bool ok;
-  const Seq s = sequence(a, b, ok);
-  if (i >= s.n || greedy(a, b)) return;
-  if (tid == 0) {   // drafts below row i, in order
-    int n = 0;
-    for (int j = i + 1; j < s.n; j++)
-      if (a.parents[s.off + j] == i && a.tokens[s.off + j] >= 0 && a.tokens[s.off + j] < a.vocab) kids[n++] = j;
-    n_kids = n;
-  }
-  __syncthreads();
-  if (n_kids < 2) return;
-  const int64_t row = s.off + i;
-  const float heat = heat_of(a, b);
-  if (!(heat > 0.f) || heat == INFINITY) return;
-  float top;
-  int arg;
-  double sum;
-  join_row(a, row, Exp(heat), tid % kWave, top, arg, sum);
-  for (int k = 0; k + 1 < n_kids; k++) {
-    double z = 1.;
-    for (int e = 0; e < k; e++) z = levels[e] == 0. ? z : levels[e];
-    double total = 0.;
-    for (int at = tid * kEach; at < a.vocab; at += kThreads * kEach) {
-      float x[kEach], d[kEach];
-      load16(a.type, a.logits, row * a.ld + at, a.vocab - at, -INFINITY, x);
-      load16(a.draft_type, a.draft, row * a.ld_draft + at, a.vocab - at, 0.f, d);
 #pragma unroll
-      for (int e = 0; e < kEach; e++)
-        total += fmax(remains(prob(a, x[e], top, sum, heat), d[e], levels, k) - static_cast<double>(d[e]), 0.);
+    for (int w = 1; w < kWaves; w++) top = fmaxf(top, tops[w]);
+    sum = 0.;
+    arg = INT32_MAX;
+    const float rate = greedy ? 0.f : rate_of(heat);
+#pragma unroll
+    for (int w = 0; w < kWaves; w++) {
+      // a wave that found nothing but -infinity has no part in the sum, or NaN
+      sum += greedy || tops[w] == top || tops[w] == -INFINITY ? sums[w] : sums[w] * __builtin_amdgcn_exp2f((tops[w] - top) * rate);
+      if (tops[w] == top) arg = min(arg, args[w]);
     }
-    total = wave_sum64(total);
-    if (tid % kWave == 0) parts[tid / kWave] = total;
-    __syncthreads();
-    if (tid == 0) {
-      levels[k] = ((parts[0] + parts[1]) + parts[2]) + parts[3];
-      a.level[s.off + kids[k]] = levels[k];
-    }
-    __syncthreads();
+    a.top[row * a.blocks + block] = top;
+    a.sum[row * a.blocks + block] = sum;
+    if (greedy) a.arg[row * a.blocks + block] = arg;
   }
 }
 
-__global__ void __launch_bounds__(kThreads) walk_kernel(Args a) {
-  __shared__ double sums[kMaxNew];
+// a row's probability of a logit, in 64 bits
+__device__ __forceinline__ double prob(double x, float top, double sum, double heat) { return exp((x - top) / heat) / sum; }
+
+// Drafts of a sequence as the walk reads them.
+struct Drafts {
+  double prob[kMaxNew];   // at the parent
+  float share[kMaxNew];   // of the draft distribution there
+  float u[kMaxNew];
+  int above[kMaxNew], token[kMaxNew];
+  double sum[kMaxNew];    // of its own row, NaN: no distribution
+};
+
+// Walks on, in one wave: to the end, or to a refusal that needs a sum.
+__device__ __forceinline__ void walk(const Args& a, int b, const Seq& s, const Drafts& d, State& st, int lane) {
+  for (;;) {
+    // the next draft below cur
+    int i = -1;
+    for (int j0 = st.at + 1; j0 < s.n && i < 0; j0 += kWave) {
+      const uint64_t kids = __ballot(j0 + lane < s.n && d.above[j0 + lane] == st.cur);
+      if (kids) i = j0 + __builtin_ctzll(kids);
+    }
+    if (i < 0) {
+      st.need = kDraw;
+      return;
+    }
+    st.at = i;
+    const double p = d.prob[i];
+    const float u = fminf(fmaxf(d.u[i], 0.f), 0x1.fffffep-1f);
+    bool yes;
+    if (a.draft) {
+      const double w = d.share[i];
+      yes = u * w * st.s < p - st.c * w;
+    } else {
+      // taken out before, by an elder sibling
+      bool again = false;
+      for (int j0 = st.cur + 1; j0 < i; j0 += kWave) {
+        const int j = j0 + lane;
+        again = again || (j < i && d.above[j] == st.cur && d.token[j] == d.token[i]);
+      }
+      again = __any(again);
+      yes = !again && u * st.s < p;
+      if (!yes && !again) st.s -= p;
+    }
+    if (yes) {
+      if (lane == 0) a.keep[static_cast<int64_t>(b) * a.max_new + st.count] = i;
+      st.cur = i;
+      st.count++;
+      st.c = 0.;
+      st.s = 1.;
+      if (d.sum[i] != d.sum[i]) {   // nothing to go on with
+        if (lane == 0) {
+          report(a, MOE_ERR_RANGE);
+          a.next[b] = -1;
+        }
+        st.need = kDone;
+        return;
+      }
+    } else if (a.draft) {
+      st.need = kRefusal;
+      return;
+    }
+  }
+}
+
+__global__ void __launch_bounds__(1024) walk_kernel(Args a) {
+  __shared__ Drafts d;
   __shared__ float tops[kMaxNew];
-  __shared__ int args[kMaxNew], parent[kMaxNew], token[kMaxNew];
-  __shared__ uint8_t yes[kMaxNew];
-  __shared__ int path[kMaxNew], n_path, last;
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid % kWave;
+  __shared__ int args[kMaxNew];
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, threads = blockDim.x;
   bool ok;
   const Seq s = sequence(a, b, ok);
   if (!ok && tid == 0) report(a, MOE_ERR_SLOT);
   const float heat = heat_of(a, b);
-  const bool first = greedy(a, b), cold = !first && (!(heat > 0.f) || heat == INFINITY);
-  const Exp ex(heat);
-  for (int i = tid / kWave; i < s.n; i += kThreads / kWave) {
-    float top;
-    int arg;
-    double sum;
-    join_row(a, s.off + i, ex, lane, top, arg, sum);
-    // not a distribution: NaN for a sum
-    if (cold || !(__builtin_fabsf(top) < INFINITY)) sum = __builtin_nan("");
-    if (lane == 0) {
-      sums[i] = sum;
-      tops[i] = top;
-      args[i] = arg;
-      a.row_sum[s.off + i] = sum;
-      a.row_top[s.off + i] = top;
-    }
-  }
-  for (int i = tid; i < s.n; i += kThreads) {
+  const bool greedy = !a.u || heat == 0.f, cold = !greedy && (!(heat > 0.f) || heat == INFINITY);
+  const float rate = greedy ? 0.f : rate_of(heat);
+  for (int i = tid; i < s.n; i += threads) {
     int p = i ? (a.parents ? a.parents[s.off + i] : i - 1) : -1;
     const int x = a.tokens[s.off + i];
     if (i && (p < -1 || p >= i || x < 0 || x >= a.vocab)) {
       report(a, MOE_ERR_SLOT);
       p = -1;
     }
-    parent[i] = p;
-    token[i] = x;
+    d.above[i] = p;
+    d.token[i] = x;
+    d.u[i] = greedy ? 0.f : a.u[s.off + i];
+    d.prob[i] = p < 0 || greedy ? 0. : load_elem(a.logits, (s.off + p) * a.ld + x, a.type);   // the logit, for now
+    d.share[i] = p < 0 || greedy || !a.draft ? 0.f : load_elem(a.draft, (s.off + p) * a.ld_draft + x, a.draft_type);
   }
-  __syncthreads();
-  for (int i = tid; i < s.n; i += kThreads) {
-    const int p = parent[i], x = token[i];
-    bool accepted = false;
-    if (p >= 0 && sums[p] == sums[p]) {
-      if (first) {
-        accepted = args[p] == x;
-      } else {
-        const float un = fminf(fmaxf(a.u[s.off + i], 0.f), 0x1.fffffep-1f);
-        const double pr = prob(a, load_elem(a.logits, (s.off + p) * a.ld + x, a.type), tops[p], sums[p], heat);
-        if (a.draft) {
-          const double d = load_elem(a.draft, (s.off + p) * a.ld_draft + x, a.draft_type);
-          double r = pr, z = 1.;   // with the sums after the elder siblings
-          for (int j = p + 1; j < i; j++)
-            if (parent[j] == p) {
-              const double level = a.level[s.off + j];
-              if (level == 0.) continue;
-              r = fmax(r / z - d, 0.);
-              z = level;
-            }
-          accepted = un * d < r / z;
-        } else {
-          double left = 1.;   // without the elder siblings
-          bool again = false;
-          for (int j = p + 1; j < i; j++)
-            if (parent[j] == p) {
-              bool seen = false;
-              for (int e = p + 1; e < j; e++) seen = seen || (parent[e] == p && token[e] == token[j]);
-              again = again || token[j] == x;
-              if (!seen) left -= prob(a, load_elem(a.logits, (s.off + p) * a.ld + token[j], a.type), tops[p], sums[p], heat);
-            }
-          accepted = !again && un * left < pr;
-        }
-      }
+  for (int i = tid; i < a.max_new; i += threads) a.keep[static_cast<int64_t>(b) * a.max_new + i] = i || s.n == 0 ? -1 : 0;
+  // rows' blocks: `wide` lanes to a row, a power of two
+  const int wide = a.blocks >= kWave ? kWave : 1 << (32 - __builtin_clz(a.blocks) - ((a.blocks & (a.blocks - 1)) == 0));
+  for (int i0 = tid / kWave * (kWave / wide); i0 < s.n; i0 += threads / wide) {
+    const int i = i0 + lane / wide, c0 = lane % wide;
+    const bool live = i < s.n;
+    const int64_t at = (s.off + i) * static_cast<int64_t>(a.blocks);
+    const float t0 = live && c0 < a.blocks ? a.top[at + c0] : -INFINITY;
+    const double z0 = live && c0 < a.blocks ? a.sum[at + c0] : 0.;
+    float top = t0;
+    for (int c = c0 + wide; live && c < a.blocks; c += wide) top = fmaxf(top, a.top[at + c]);
+    for (int w = wide / 2; w; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
+    auto part = [&](float t, double z) {
+      return greedy || t == top || t == -INFINITY ? z : z * static_cast<double>(__builtin_amdgcn_exp2f((t - top) * rate));
+    };
+    double sum = part(t0, z0);
+    int arg = greedy && live && c0 < a.blocks && t0 == top ? a.arg[at + c0] : INT32_MAX;
+    for (int c = c0 + wide; live && c < a.blocks; c += wide) {
+      const float t = a.top[at + c];
+      sum += part(t, a.sum[at + c]);
+      if (greedy && t == top) arg = min(arg, a.arg[at + c]);
     }
-    yes[i] = accepted;
-  }
-  __syncthreads();
-  if (tid == 0) {
-    int n = 0, cur = 0;
-    if (s.n > 0) path[n++] = 0;
-    for (int i = 1; i < s.n; i++)
-      if (parent[i] == cur && yes[i]) path[n++] = cur = i;
-    const bool none = s.n > 0 && sums[cur] != sums[cur];
-    if (none) report(a, MOE_ERR_RANGE);
-    n_path = n;
-    a.n_keep[b] = n;
-    a.end[b] = s.n == 0 || none || first ? -1 : cur;
-    if (s.n == 0 || none) a.next[b] = -1;
-    else if (first) a.next[b] = args[cur];
-  }
-  __syncthreads();
-  for (int j = tid; j < a.max_new; j += kThreads) a.keep[static_cast<int64_t>(b) * a.max_new + j] = j < n_path ? path[j] : -1;
-}
-
-// What there is to draw from at the end of a walk.
-struct Rest {
-  int64_t row;
-  int n;         // refused drafts
-  float top;
-  double sum, heat;
-};
-struct RestLds {
-  int token[kMaxNew];
-  double level[kMaxNew];
-  int n;
-};
-
-__device__ __forceinline__ Rest rest_of(const Args& a, int b, const Seq& s, int cur, RestLds& lds, int tid) {
-  Rest r;
-  r.row = s.off + cur;
-  r.top = a.row_top[r.row];
-  r.sum = a.row_sum[r.row];
-  r.heat = heat_of(a, b);
-  if (tid == 0) {
-    int n = 0;
-    for (int j = cur + 1; j < s.n; j++) {
-      const int p = a.parents ? a.parents[s.off + j] : j - 1, x = a.tokens[s.off + j];
-      if (p != cur || x < 0 || x >= a.vocab) continue;
-      lds.token[n] = x;
-      lds.level[n++] = a.draft && a.parents ? a.level[s.off + j] : 0.;   // not set for the last one
+    for (int w = wide / 2; w; w >>= 1) {
+      sum += __shfl_xor(sum, w);
+      arg = min(arg, __shfl_xor(arg, w));
     }
-    lds.n = n;
-  }
-  __syncthreads();
-  r.n = lds.n;
-  return r;
-}
-
-// 16 tokens' shares from `at` on, after `n` refusals
-__device__ __forceinline__ void shares(const Args& a, const Rest& r, const RestLds& lds, int n, int at, double (&v)[kEach]) {
-  float x[kEach];
-  load16(a.type, a.logits, r.row * a.ld + at, a.vocab - at, -INFINITY, x);
-#pragma unroll
-  for (int e = 0; e < kEach; e++) v[e] = exp((static_cast<double>(x[e]) - r.top) / r.heat);
-  if (n == 0) return;
-  if (a.draft) {
-    float d[kEach];
-    load16(a.draft_type, a.draft, r.row * a.ld_draft + at, a.vocab - at, 0.f, d);
-#pragma unroll
-    for (int e = 0; e < kEach; e++) v[e] = fmax(remains(v[e] / r.sum, d[e], lds.level, n - 1) - static_cast<double>(d[e]), 0.);
-  } else {
-    for (int k = 0; k < n; k++) {
-      const int e0 = lds.token[k] - at;
-#pragma unroll
-      for (int e = 0; e < kEach; e++) v[e] = e == e0 ? 0. : v[e];
+    // not a distribution: NaN for a sum
+    if (cold || !(__builtin_fabsf(top) < INFINITY)) sum = __builtin_nan("");
+    if (live && c0 == 0) {
+      d.sum[i] = sum;
+      tops[i] = top;
+      args[i] = arg;
+      a.row_sum[s.off + i] = sum;
+      a.row_top[s.off + i] = top;
     }
   }
-}
-
-__device__ __forceinline__ double block_sum(double v, double* parts, int tid) {
-  v = wave_sum64(v);
   __syncthreads();
-  if (tid % kWave == 0) parts[tid / kWave] = v;
-  __syncthreads();
-  return ((parts[0] + parts[1]) + parts[2]) + parts[3];
-}
-
-__global__ void __launch_bounds__(kThreads) total_kernel(Args a) {
-  __shared__ RestLds lds;
-  __shared__ double parts[kThreads / kWave];
-  const int chunk = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
-  const int cur = a.end[b];
-  if (cur < 0) return;
-  bool ok;
-  const Seq s = sequence(a, b, ok);
-  const Rest r = rest_of(a, b, s, cur, lds, tid);
-  double v[kEach];
-  shares(a, r, lds, r.n, chunk * kChunk + tid * kEach, v);
-  double t = 0.;
-#pragma unroll
-  for (int e = 0; e < kEach; e++) t += v[e];
-  t = block_sum(t, parts, tid);
-  if (tid == 0) a.total[static_cast<int64_t>(b) * a.chunks + chunk] = t;
-}
-
-__global__ void __launch_bounds__(kThreads) pick_kernel(Args a) {
-  __shared__ RestLds lds;
-  __shared__ double parts[kThreads / kWave], sums[kThreads];
-  __shared__ int found;
-  const int b = blockIdx.x, tid = threadIdx.x;
-  const int cur = a.end[b];
-  if (cur < 0) return;
-  bool ok;
-  const Seq s = sequence(a, b, ok);
-  const Rest r = rest_of(a, b, s, cur, lds, tid);
-  double* total = a.total + static_cast<int64_t>(b) * a.chunks;
-  int n = r.n;
-  double all;
-  for (;;) {
-    double t = 0.;
-    for (int c = tid; c < a.chunks; c += kThreads) t += total[c];
-    all = block_sum(t, parts, tid);
-    if (all > 0. || n == 0) break;
-    n--;    // nothing remains after the last refusal: what there was before it
-    for (int c = 0; c < a.chunks; c++) {
-      double v[kEach], sum = 0.;
-      shares(a, r, lds, n, c * kChunk + tid * kEach, v);
-#pragma unroll
-      for (int e = 0; e < kEach; e++) sum += v[e];
-      sum = block_sum(sum, parts, tid);
-      if (tid == 0) total[c] = sum;
+  if (!greedy) {
+    for (int i = tid; i < s.n; i += threads) {
+      const int p = d.above[i];
+      if (p >= 0) d.prob[i] = prob(d.prob[i], tops[p], d.sum[p], heat);
+      a.prob[s.off + i] = d.prob[i];
+      a.share[s.off + i] = d.share[i];
+      a.above[s.off + i] = p;
     }
     __syncthreads();
   }
-  const double aim = static_cast<double>(fminf(fmaxf(a.u_next[b], 0.f), 0x1.fffffep-1f)) * all;
-  // the chunk: the first whose end passes the aim, or the last that has anything
-  if (tid == 0) {
-    double up = 0., before = 0.;
-    int at = 0;
-    for (int c = 0; c < a.chunks; c++) {
-      const double t = total[c];
-      if (t > 0.) {
-        at = c;
-        before = up;
+  if (tid >= kWave) return;
+  State st{0., 1., 0., 0.f, 0, 0, s.n > 0, kDone};
+  if (s.n == 0 || d.sum[0] != d.sum[0]) {
+    if (lane == 0) {
+      if (s.n) report(a, MOE_ERR_RANGE);
+      a.next[b] = -1;
+    }
+  } else if (greedy) {
+    for (int j0 = 1; j0 < s.n;) {   // drafts below cur whose token is the largest
+      const int j = j0 + lane;
+      const uint64_t kids = __ballot(j < s.n && d.above[j] == st.cur && d.token[j] == args[st.cur]);
+      if (!kids) {
+        j0 += kWave;
+        continue;
       }
-      up += t;
-      if (up > aim) break;
+      st.cur = j0 + __builtin_ctzll(kids);
+      if (lane == 0) a.keep[static_cast<int64_t>(b) * a.max_new + st.count] = st.cur;
+      st.count++;
+      j0 = st.cur + 1;
+      if (d.sum[st.cur] != d.sum[st.cur]) break;
     }
-    found = at;
-    parts[0] = before;
+    if (lane == 0) {
+      const bool none = d.sum[st.cur] != d.sum[st.cur];
+      if (none) report(a, MOE_ERR_RANGE);
+      a.next[b] = none ? -1 : args[st.cur];
+    }
+  } else {
+    walk(a, b, s, d, st, lane);
+    st.sum = d.sum[st.cur];
+    st.top = tops[st.cur];
   }
-  __syncthreads();
-  const int at = found * kChunk + tid * kEach;
-  const double before = parts[0];
-  double v[kEach], sum = 0.;
-  shares(a, r, lds, n, at, v);
-#pragma unroll
-  for (int e = 0; e < kEach; e++) sum += v[e];
-  sums[tid] = sum;
-  __syncthreads();
-  if (tid == 0) {
-    double up = before, mine = before;
-    int t = 0;
-    for (int i = 0; i < kThreads; i++) {
-      if (sums[i] > 0.) {
-        t = i;
-        mine = up;
-      }
-      up += sums[i];
-      if (up > aim) break;
-    }
-    found = t;
-    parts[0] = mine;
-  }
-  __syncthreads();
-  if (tid == found) {
-    double up = parts[0];
-    int x = 0;
-    bool done = false;
-#pragma unroll
-    for (int e = 0; e < kEach; e++) {
-      if (!done && v[e] > 0.) x = e;
-      up += v[e];
-      done = done || up > aim;
-    }
-    a.next[b] = at + x;
+  if (lane == 0) {
+    a.n_keep[b] = st.count;
+    a.state[b] = st;
+    a.arrived[b] = 0;
   }
 }
 
+// What one row's pass sums up, and the last one draws from.
+struct Row {
+  int64_t row;
+  float top;
+  double sum, heat, c;
+};
+
+struct Taken {
+  int n, token[kMaxNew];
+};
+
+// a thread's tokens' parts, from `at` on
+__device__ __forceinline__ void parts_of(const Args& a, const Row& r, const Taken& out, int at, double (&v)[kEach]) {
+  float x[kEach], w[kEach];
+  load_some(a.type, a.logits, r.row * a.ld + at, a.vocab - at, -INFINITY, x);
+  if (r.c > 0.) load_some(a.draft_type, a.draft, r.row * a.ld_draft + at, a.vocab - at, 0.f, w);
+  const double inv = 1. / r.heat;
+#pragma unroll
+  for (int e = 0; e < kEach; e++) v[e] = exp((static_cast<double>(x[e]) - r.top) * inv);
+  if (r.c > 0.) {
+    const double scale = 1. / r.sum;
+#pragma unroll
+    for (int e = 0; e < kEach; e++) v[e] = fmax(v[e] * scale - r.c * static_cast<double>(w[e]), 0.);
+  }
+  for (int k = 0; !a.draft && k < out.n; k++) {
+    const int e0 = out.token[k] - at;
+#pragma unroll
+    for (int e = 0; e < kEach; e++) v[e] = e == e0 ? 0. : v[e];
+  }
+}
+
+// inclusive sum over the threads before and at this one; `all` the sum of all
+__device__ __forceinline__ double scan(double v, double* lds, int tid, double& all) {
+  const int lane = tid % kWave, wave = tid / kWave;
+  for (int w = 1; w < kWave; w <<= 1) {
+    const double t = __shfl_up(v, w);
+    v += lane >= w ? t : 0.;
+  }
+  __syncthreads();
+  if (lane == kWave - 1) lds[wave] = v;
+  __syncthreads();
+  double before = 0.;
+  all = 0.;
+  for (int w = 0; w < kWaves; w++) {
+    if (w < wave) before += lds[w];
+    all += lds[w];
+  }
+  return before + v;
+}
+
+// Of the threads that have something, the first whose inclusive sum passes the aim, or the last
+__device__ __forceinline__ int first_past(double mine, double up, double aim, int* lds, int tid) {
+  const int wave = tid / kWave;
+  const uint64_t past = __ballot(mine > 0. && up > aim), some = __ballot(mine > 0.);
+  __syncthreads();
+  if (tid % kWave == 0) {
+    lds[2 * wave] = past ? wave * kWave + __builtin_ctzll(past) : -1;
+    lds[2 * wave + 1] = some ? wave * kWave + 63 - __builtin_clzll(some) : -1;
+  }
+  __syncthreads();
+  int at = 0;
+  for (int w = 0; w < kWaves; w++)
+    if (lds[2 * w + 1] >= 0) at = lds[2 * w + 1];
+  for (int w = kWaves - 1; w >= 0; w--)
+    if (lds[2 * w] >= 0) at = lds[2 * w];
+  return at;
+}
+
+// sums that one workgroup of a launch writes and another reads
+__device__ __forceinline__ void put_total(double* p, double v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ double read_total(const double* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+__global__ void __launch_bounds__(kThreads) pass_kernel(Args a, int last) {
+  __shared__ Taken taken;
+  __shared__ Drafts d;
+  __shared__ double parts[kWaves], carry;
+  __shared__ int marks[2 * kWaves], chosen;
+  __shared__ State shared;
+  const int chunk = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid % kWave;
+  State st = a.state[b];
+  if (st.need == kDone) return;
+  bool ok;
+  const Seq s = sequence(a, b, ok);
+  Row r;
+  r.heat = heat_of(a, b);
+  // what to sum next: sets r, and the tokens that are taken out of cur's row
+  auto aim_at = [&]() {
+    r.row = s.off + st.cur;
+    r.top = st.top;
+    r.sum = st.sum;
+    r.c = a.draft ? st.need == kRefusal ? st.c + st.s : st.c : 0.;
+    if (a.draft) return;
+    __syncthreads();
+    if (tid == 0) taken.n = 0;
+    __syncthreads();
+    if (st.s > 0.)
+      for (int j = st.cur + 1 + tid; j < s.n; j += kThreads)
+        if (a.above[s.off + j] == st.cur) taken.token[atomicAdd(&taken.n, 1)] = a.tokens[s.off + j];
+    __syncthreads();
+  };
+  auto chunk_sum = [&](int c) {
+    double v[kEach], t = 0.;
+    parts_of(a, r, taken, c * kChunk + tid * kEach, v);
+#pragma unroll
+    for (int e = 0; e < kEach; e++) t += v[e];
+    t = wave_sum64(t);
+    __syncthreads();
+    if (lane == 0) parts[tid / kWave] = t;
+    __syncthreads();
+    return ((parts[0] + parts[1]) + parts[2]) + parts[3];
+  };
+  double* total = a.total + static_cast<int64_t>(b) * a.chunks;
+  aim_at();
+  const double mine = chunk_sum(chunk);
+  if (tid == 0) {
+    put_total(&total[chunk], mine);
+    // All that workgroups of one launch hand over is that sum, stored past the XCD's L2: once it has
+    // arrived, the count may go up.  (A release at device scope writes the whole L2 back, for each
+    // workgroup: 64 sequences by 32 chunks 46 us that way.)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    chosen = __hip_atomic_fetch_add(&a.arrived[b], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!chosen) return;
+  // the last workgroup of the sequence: add up, and walk on
+  if (tid == 0) a.arrived[b] = 0;
+  for (int i = tid; i < s.n; i += kThreads) {
+    d.prob[i] = a.prob[s.off + i];
+    d.share[i] = a.share[s.off + i];
+    d.u[i] = a.u[s.off + i];
+    d.above[i] = a.above[s.off + i];
+    d.token[i] = a.tokens[s.off + i];
+    d.sum[i] = a.row_sum[s.off + i];
+  }
+  __syncthreads();
+  const int each = (a.chunks + kThreads - 1) / kThreads;   // chunks of a thread, side by side
+  for (bool summed = true;;) {
+    if (!summed) {   // alone, chunk after chunk
+      aim_at();
+      for (int c = 0; c < a.chunks; c++) {
+        const double t = chunk_sum(c);
+        if (tid == 0) put_total(&total[c], t);
+      }
+      __syncthreads();
+    }
+    double have = 0., all;
+    for (int c = tid * each; c < min((tid + 1) * each, a.chunks); c++) have += read_total(&total[c]);
+    const double up = scan(have, parts, tid, all);
+    const int need = st.need;
+    bool draw = need == kDraw;
+    if (need == kRefusal) {
+      const int row = st.cur;
+      if (all > 0.) {    // nothing left: as if it had not been refused
+        st.c = r.c;
+        st.s = all;
+      }
+      if (tid < kWave) {
+        walk(a, b, s, d, st, lane);
+        if (lane == 0) {
+          shared = st;
+          shared.sum = d.sum[st.cur];
+          shared.top = a.row_top[s.off + st.cur];
+        }
+      }
+      __syncthreads();
+      st = shared;
+      __syncthreads();
+      draw = st.need == kDraw && st.cur == row && all > 0.;    // these very sums are drawn from
+    } else if (!(all > 0.) && (a.draft ? st.c > 0. : taken.n > 0)) {   // nothing left in 64 bits: the whole row
+      st.c = 0.;
+      st.s = -1.;
+      draw = false;
+    }
+    if (draw) {
+      const double goal = static_cast<double>(fminf(fmaxf(a.u_next[b], 0.f), 0x1.fffffep-1f)) * all;
+      const int t = first_past(have, up, goal, marks, tid);
+      if (tid == t) {    // the chunk among this thread's
+        double before = up - have;
+        int at = t * each;
+        for (int c = t * each; c < min((t + 1) * each, a.chunks); c++) {
+          const double part = read_total(&total[c]);
+          if (part > 0.) {
+            at = c;
+            carry = before;
+          }
+          before += part;
+          if (part > 0. && before > goal) break;
+        }
+        chosen = at;
+      }
+      __syncthreads();
+      const int at = chosen * kChunk + tid * kEach;
+      const double before = carry;
+      double v[kEach], have2 = 0., all2;
+      parts_of(a, r, taken, at, v);
+#pragma unroll
+      for (int e = 0; e < kEach; e++) have2 += v[e];
+      const double up2 = before + scan(have2, parts, tid, all2);
+      if (tid == first_past(have2, up2, goal, marks, tid)) {
+        double sum = up2 - have2;
+        int x = 0;
+        bool done = false;
+#pragma unroll
+        for (int e = 0; e < kEach; e++) {
+          if (!done && v[e] > 0.) x = e;
+          sum += v[e];
+          done = done || (v[e] > 0. && sum > goal);
+        }
+        a.next[b] = at + x;
+      }
+      st.need = kDone;
+    }
+    if (st.need == kDone || !last) break;
+    summed = false;
+  }
+  if (tid == 0) {
+    a.n_keep[b] = st.count;
+    a.state[b] = st;
+  }
+}
+
+// Statistics of a row by blocks of 16 or, where there are enough of them to fill the card twice, 32
+// tokens a thread.
+int each_of(int64_t n_tokens, int64_t vocab) { return n_tokens * cdiv(vocab, 16 * kThreads) > 2048 ? 32 : 16; }
+
 struct Layout {
-  int64_t chunks;
-  size_t sum, level, row_sum, total, top, row_top, arg, end, bytes;
+  int64_t blocks, chunks;
+  size_t sum, total, row_sum, prob, state, top, row_top, share, arg, above, arrived, bytes;
 };
 Layout layout_of(int64_t n_seqs, int64_t n_tokens, int64_t vocab) {
   Layout l;
+  l.blocks = cdiv(vocab, each_of(n_tokens, vocab) * kThreads);
   l.chunks = cdiv(vocab, kChunk);
   size_t at = 0;
   auto put = [&](size_t bytes) {
@@ -518,16 +593,26 @@ Layout layout_of(int64_t n_seqs, int64_t n_tokens, int64_t vocab) {
     at += (bytes + 15) / 16 * 16;
     return here;
   };
-  l.sum = put(8 * n_tokens * l.chunks);
-  l.level = put(8 * n_tokens);
-  l.row_sum = put(8 * n_tokens);
+  l.sum = put(8 * n_tokens * l.blocks);
   l.total = put(8 * n_seqs * l.chunks);
-  l.top = put(4 * n_tokens * l.chunks);
+  l.row_sum = put(8 * n_tokens);
+  l.prob = put(8 * n_tokens);
+  l.state = put(sizeof(State) * n_seqs);
+  l.top = put(4 * n_tokens * l.blocks);
   l.row_top = put(4 * n_tokens);
-  l.arg = put(4 * n_tokens * l.chunks);
-  l.end = put(4 * n_seqs);
+  l.share = put(4 * n_tokens);
+  l.arg = put(4 * n_tokens * l.blocks);
+  l.above = put(4 * n_tokens);
+  l.arrived = put(4 * n_seqs);
   l.bytes = at;
   return l;
+}
+
+template <int TYPE>
+void launch_stats(bool wide, int most, hipStream_t s, const Args& a) {
+  const dim3 grid(a.blocks, most, a.n_seqs), block(kThreads);
+  if (wide) hipLaunchKernelGGL((stats_kernel<TYPE, 32>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((stats_kernel<TYPE, 16>), grid, block, 0, s, a);
 }
 
 int check_sizes(int32_t n_seqs, int32_t n_tokens, int32_t max_new, int32_t vocab) {
@@ -581,22 +666,54 @@ extern "C" int moe_draft_verify(const void* logits, int32_t logits_type, int64_t
   }
   char* w = static_cast<char*>(ws);
   auto part = [&](size_t at) { return static_cast<void*>(w + at); };
-  const Args a{logits, draft, tokens, parents, new_off, temperature, u, u_next, keep, n_keep, next, status,
-               static_cast<double*>(part(l.sum)), static_cast<double*>(part(l.level)), static_cast<double*>(part(l.total)),
-               static_cast<float*>(part(l.top)), static_cast<int32_t*>(part(l.arg)), static_cast<int32_t*>(part(l.end)),
-               static_cast<double*>(part(l.row_sum)), static_cast<float*>(part(l.row_top)), ld_logits, ld_draft,
-               n_seqs, n_tokens, max_new, vocab, static_cast<int>(l.chunks), logits_type, draft_type};
+  Args a;
+  a.logits = logits;
+  a.draft = draft;
+  a.tokens = tokens;
+  a.parents = parents;
+  a.off = new_off;
+  a.temperature = temperature;
+  a.u = u;
+  a.u_next = u_next;
+  a.keep = keep;
+  a.n_keep = n_keep;
+  a.next = next;
+  a.status = status;
+  a.sum = static_cast<double*>(part(l.sum));
+  a.total = static_cast<double*>(part(l.total));
+  a.row_sum = static_cast<double*>(part(l.row_sum));
+  a.prob = static_cast<double*>(part(l.prob));
+  a.top = static_cast<float*>(part(l.top));
+  a.row_top = static_cast<float*>(part(l.row_top));
+  a.share = static_cast<float*>(part(l.share));
+  a.arg = static_cast<int32_t*>(part(l.arg));
+  a.above = static_cast<int32_t*>(part(l.above));
+  a.state = static_cast<State*>(part(l.state));
+  a.arrived = static_cast<unsigned*>(part(l.arrived));
+  a.ld = ld_logits;
+  a.ld_draft = ld_draft;
+  a.n_seqs = n_seqs;
+  a.n_tokens = n_tokens;
+  a.max_new = max_new;
+  a.vocab = vocab;
+  a.blocks = static_cast<int>(l.blocks);
+  a.chunks = static_cast<int>(l.chunks);
+  a.type = logits_type;
+  a.draft_type = draft_type;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int most = std::min(max_new, n_tokens);
-  const unsigned chunks = static_cast<unsigned>(l.chunks);
+  const dim3 block(kThreads);
   if (most > 0) {
-    hipLaunchKernelGGL(stats_kernel, dim3(chunks, most, n_seqs), dim3(kThreads), 0, s, a);
-    if (draft && parents && u) hipLaunchKernelGGL(level_kernel, dim3(most, n_seqs), dim3(kThreads), 0, s, a);
+    const bool wide = each_of(n_tokens, vocab) == 32;
+    if (logits_type == MOE_TYPE_FP32) launch_stats<MOE_TYPE_FP32>(wide, most, s, a);
+    else if (logits_type == MOE_TYPE_BF16) launch_stats<MOE_TYPE_BF16>(wide, most, s, a);
+    else launch_stats<MOE_TYPE_FP16>(wide, most, s, a);
   }
-  hipLaunchKernelGGL(walk_kernel, dim3(n_seqs), dim3(kThreads), 0, s, a);
+  // a lane for every block of a sequence's rows, if that takes no more than a workgroup
+  hipLaunchKernelGGL(walk_kernel, dim3(n_seqs), dim3(static_cast<int64_t>(most) * a.blocks > kThreads ? 1024 : kThreads), 0, s, a);
   if (most > 0 && u) {
-    hipLaunchKernelGGL(total_kernel, dim3(chunks, n_seqs), dim3(kThreads), 0, s, a);
-    hipLaunchKernelGGL(pick_kernel, dim3(n_seqs), dim3(kThreads), 0, s, a);
+    const int passes = draft && parents ? std::min(kPasses, most) : 1;
+    for (int i = 0; i < passes; i++) hipLaunchKernelGGL(pass_kernel, dim3(a.chunks, n_seqs), block, 0, s, a, i == passes - 1);
   }
   return launch_status(s);
 }
