@@ -96,10 +96,24 @@ __device__ __forceinline__ uint32_t codes4(const float* f, float s, float inv) {
   return lo | hi;
 }
 
-// One workgroup per 64 aligned slots of a sequence and key/value head g, laid out as the plain
-// append's: a thread has one pair of 8-channel chunks of one token, the chunks that turn
-// together, and D / 16 lanes side by side have a head, so that norm and largest magnitude are
-// sums and maxima over a few lanes.
+// N floats of a row, at any address of one
+template <int N>
+__device__ __forceinline__ void load_floats(const float* p, float* f) {
+  struct __attribute__((packed, aligned(4))) Four { float w[4]; };
+#pragma unroll
+  for (int i = 0; i < N / 4; i++) {
+    const Four x = reinterpret_cast<const Four*>(p)[i];
+#pragma unroll
+    for (int e = 0; e < 4; e++) f[4 * i + e] = x.w[e];
+  }
+}
+
+// One workgroup per 64 aligned slots of a sequence and key/value head g.  D / 16 lanes side by
+// side take a head of one token, each a pair of its 8-channel chunks, the chunks that turn
+// together, so that norm and largest magnitude are sums and maxima over a few lanes.  The
+// tile's live tokens times its heads (the key's and the queries') are dealt out over the
+// workgroup: a tree of few tokens has its heads side by side.  What the row's place alone tells is on
+// its way before positions and pages are known, and the next head's row during this one's arithmetic.
 template <int TYPE, int D, bool Q8>
 __global__ void __launch_bounds__(4 * D) store_kernel(StoreArgs a) {
   typedef elem_t<TYPE> E;
@@ -120,12 +134,39 @@ __global__ void __launch_bounds__(4 * D) store_kernel(StoreArgs a) {
   if (first >= end) return;
   const int slot0 = static_cast<int>(first);
   const int64_t t0 = static_cast<int64_t>(q.off) - q.len + slot0;   // token of the tile's first slot
+  auto live = [&](int o) { return slot0 + o >= q.len && slot0 + o < end; };
+
+  // values: each thread two slots by 8 channels
+  const int vc8 = tid % (D / 8) * 8, pair = tid / (D / 8);
+  Piece val[2] = {};
+#pragma unroll
+  for (int e = 0; e < 2; e++)
+    if (live(2 * pair + e))
+      val[e] = *reinterpret_cast<const Piece*>(static_cast<const E*>(a.v) + (t0 + 2 * pair + e) * a.ld_v + g * D + vc8);
+  // keys and queries
+  const int half = a.rot_dim / 2, j = tid % kItems;
+  const bool turn = a.cos && 16 * j < a.rot_dim;
+  const bool split = turn && !a.interleaved;    // chunks half a rotation apart
+  const int c0 = split ? 8 * j : 16 * j, c1 = split ? half + 8 * j : 16 * j + 8;
+  const int o_first = max(q.len - slot0, 0), n_live = min(end - slot0, kSlots) - o_first;
+  const int items = n_live * (a.q ? a.group + 1 : 1);   // item i: head i / n_live (0 the key's) of live token i % n_live
+  Piece x = {}, y = {};
+  auto load_item = [&](int i) {
+    const int head = i / n_live;
+    const int64_t t = t0 + o_first + (i - head * n_live);
+    const E* p = head == 0 ? static_cast<const E*>(a.k) + t * a.ld_k + g * D
+                           : static_cast<const E*>(a.q) + t * a.ld_q + (static_cast<int64_t>(g) * a.group + head - 1) * D;
+    x = *reinterpret_cast<const Piece*>(p + c0);
+    y = *reinterpret_cast<const Piece*>(p + c1);
+  };
+  int item = tid / kItems;
+  if (item < items) load_item(item);
+
   if (tid < kSlots) {
     const int slot = slot0 + tid;
-    const bool live = slot >= q.len && slot < end;
-    const int pos = !live ? -1 : (a.positions ? a.positions[t0 + tid] : slot);
-    const bool bad = live && a.cos && (pos < 0 || pos >= a.max_pos);
-    where[tid] = live && !bad ? (a.cos ? pos : 0) : -1;
+    const int pos = !live(tid) ? -1 : (a.positions ? a.positions[t0 + tid] : slot);
+    const bool bad = live(tid) && a.cos && (pos < 0 || pos >= a.max_pos);
+    where[tid] = live(tid) && !bad ? (a.cos ? pos : 0) : -1;
     bool lost = false;
     if (tid % 32 == 0) {
       const int page = slot < end && slot + 32 > q.len ? page_of(a.b, s, slot) : 0;
@@ -136,81 +177,66 @@ __global__ void __launch_bounds__(4 * D) store_kernel(StoreArgs a) {
   }
   __syncthreads();
 
-  // values: each thread two slots by 8 channels
-  const int vc8 = tid % (D / 8) * 8, pair = tid / (D / 8);
-  Piece val[2] = {};
-#pragma unroll
-  for (int e = 0; e < 2; e++)
-    if (where[2 * pair + e] >= 0)
-      val[e] = *reinterpret_cast<const Piece*>(static_cast<const E*>(a.v) + (t0 + 2 * pair + e) * a.ld_v + g * D + vc8);
-
-  // keys and queries: each thread one token's pair of chunks, of every head of the group
-  const int half = a.rot_dim / 2, j = tid % kItems, o = tid / kItems, pos = where[o];
-  if (pos >= 0) {
-    const int64_t t = t0 + o;
-    const bool turn = a.cos && 16 * j < a.rot_dim;
-    const bool split = turn && !a.interleaved;    // chunks half a rotation apart
-    const int c0 = split ? 8 * j : 16 * j, c1 = split ? half + 8 * j : 16 * j + 8;
-    float cs[8], sn[8];
-    if (turn) {
+  float cs[8], sn[8], w[16];     // of the last token, and of the last head's kind
+  int o_of = -1, kind_of = -1;
+  for (; item < items; item += kSlots) {
+    const int head = item / n_live, o = o_first + (item - head * n_live), pos = where[o], kind = head > 0;
+    float f[16];
+    unpack<TYPE>(x, f);
+    unpack<TYPE>(y, f + 8);
+    if (item + kSlots < items) load_item(item + kSlots);
+    if (pos < 0) continue;
+    if (turn && o != o_of) {
       const int64_t at = static_cast<int64_t>(pos) * half + 8 * j;
+      load_floats<8>(a.cos + at, cs);
+      load_floats<8>(a.sin + at, sn);
+      o_of = o;
+    }
+    if (const float* from = head ? a.w_q : a.w_k) {
+      if (kind != kind_of) {
+        load_floats<8>(from + c0, w);
+        load_floats<8>(from + c1, w + 8);
+        kind_of = kind;
+      }
+      float ss = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; e++) {
-        cs[e] = a.cos[at + e];
-        sn[e] = a.sin[at + e];
+      for (int e = 0; e < 16; e++) ss = __fmaf_rn(f[e], f[e], ss);
+      const float r = __builtin_amdgcn_rsqf(group_sum<kItems>(ss) * (1.0f / D) + a.eps);
+#pragma unroll
+      for (int e = 0; e < 16; e++) f[e] = f[e] * r * w[e];
+    }
+    if (turn) {
+      auto rotated = [&](float& u, float& v, int e) {
+        const float s = __fmaf_rn(u, cs[e], -(v * sn[e])), t = __fmaf_rn(u, sn[e], v * cs[e]);
+        u = s;
+        v = t;
+      };
+      if (a.interleaved) {
+#pragma unroll
+        for (int e = 0; e < 8; e++) rotated(f[2 * e], f[2 * e + 1], e);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++) rotated(f[e], f[8 + e], e);
       }
     }
-    auto normed_turned = [&](float (&f)[16], const float* w) {
-      if (w) {
-        float ss = 0.f;
-#pragma unroll
-        for (int e = 0; e < 16; e++) ss = __fmaf_rn(f[e], f[e], ss);
-        const float r = 1.0f / sqrtf(group_sum<kItems>(ss) * (1.0f / D) + a.eps);
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-          f[e] = f[e] * r * w[c0 + e];
-          f[8 + e] = f[8 + e] * r * w[c1 + e];
-        }
-      }
-      if (!turn) return;
-#pragma unroll
-      for (int e = 0; e < 8; e++) {
-        float &x = split ? f[e] : f[2 * e], &y = split ? f[8 + e] : f[2 * e + 1];
-        const float u = __fmaf_rn(x, cs[e], -(y * sn[e])), v = __fmaf_rn(x, sn[e], y * cs[e]);
-        x = u;
-        y = v;
-      }
-    };
-    auto both = [&](const void* base, int64_t at, float (&f)[16]) {
-      const E* p = static_cast<const E*>(base) + at;
-      unpack<TYPE>(*reinterpret_cast<const Piece*>(p + c0), f);
-      unpack<TYPE>(*reinterpret_cast<const Piece*>(p + c1), f + 8);
-    };
-    float f[16];
-    for (int h = 0; h < (a.q ? a.group : 0); h++) {
-      const int64_t c = (static_cast<int64_t>(g) * a.group + h) * D;
-      both(a.q, t * a.ld_q + c, f);
-      normed_turned(f, a.w_q);
-      E* op = static_cast<E*>(a.q_out) + t * a.ld_q_out + c;
+    if (head) {
+      E* op = static_cast<E*>(a.q_out) + (t0 + o) * a.ld_q_out + (static_cast<int64_t>(g) * a.group + head - 1) * D;
       *reinterpret_cast<Piece*>(op + c0) = packed<TYPE>(f);
       *reinterpret_cast<Piece*>(op + c1) = packed<TYPE>(f + 8);
+      continue;
     }
-    both(a.k, t * a.ld_k + g * D, f);
-    normed_turned(f, a.w_k);
-    const int64_t page = pages[o / 32];
-    if (page >= 0) {
-      const int64_t slot = page + o % 32;
-      if constexpr (Q8) {
-        const float s = scale_of(group_max<kItems>(largest<16>(f))), inv = 1.0f / s;
-        if (j == 0) a.ks[slot] = s;
-        uint8_t* out = static_cast<uint8_t*>(a.kc) + slot * D;
-        *reinterpret_cast<u32x2*>(out + c0) = u32x2{codes4(f, s, inv), codes4(f + 4, s, inv)};
-        *reinterpret_cast<u32x2*>(out + c1) = u32x2{codes4(f + 8, s, inv), codes4(f + 12, s, inv)};
-      } else {
-        E* out = static_cast<E*>(a.kc) + slot * D;
-        *reinterpret_cast<Piece*>(out + c0) = packed<TYPE>(f);
-        *reinterpret_cast<Piece*>(out + c1) = packed<TYPE>(f + 8);
-      }
+    const int64_t page = pages[o / 32], slot = page + o % 32;
+    if (page < 0) continue;
+    if constexpr (Q8) {
+      const float s = scale_of(group_max<kItems>(largest<16>(f))), inv = 1.0f / s;
+      if (j == 0) a.ks[slot] = s;
+      uint8_t* out = static_cast<uint8_t*>(a.kc) + slot * D;
+      *reinterpret_cast<u32x2*>(out + c0) = u32x2{codes4(f, s, inv), codes4(f + 4, s, inv)};
+      *reinterpret_cast<u32x2*>(out + c1) = u32x2{codes4(f + 8, s, inv), codes4(f + 12, s, inv)};
+    } else {
+      E* out = static_cast<E*>(a.kc) + slot * D;
+      *reinterpret_cast<Piece*>(out + c0) = packed<TYPE>(f);
+      *reinterpret_cast<Piece*>(out + c1) = packed<TYPE>(f + 8);
     }
   }
 
@@ -270,8 +296,15 @@ __global__ void __launch_bounds__(4 * D) store_kernel(StoreArgs a) {
       *reinterpret_cast<u32x4*>(out) = w;
     } else {
 #pragma unroll
-      for (int e = 0; e < kPiece; e++)
-        if (where[o + e] >= 0) out[e] = from[e];
+      for (int w = 0; w < kPiece; w += kPer) {    // words whose slots are all new, or their slots
+        bool word = true;
+#pragma unroll
+        for (int e = 0; e < kPer; e++) word = word && where[o + w + e] >= 0;
+        if (word) *reinterpret_cast<uint32_t*>(out + w) = *reinterpret_cast<const uint32_t*>(from + w);
+#pragma unroll
+        for (int e = 0; e < kPer; e++)
+          if (!word && where[o + w + e] >= 0) out[w + e] = from[w + e];
+      }
     }
   }
 }

@@ -23,10 +23,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
-constexpr int kChunk = 1024;        // tokens of the vocabulary of a pass's workgroup
-constexpr int kEach = kChunk / kThreads;
 constexpr int kMaxNew = 1024;
 constexpr int kPasses = 4;
+constexpr int kApart = 32;          // counters to a cache line of their own: the card takes one count a line at a time
 
 // Where a sequence's walk stands.
 struct State {
@@ -36,6 +35,7 @@ struct State {
   int cur, at;      // the row, and the last draft that was tested
   int count;        // kept rows
   int need;         // what a pass has to sum: nothing any more, a refusal, or what is drawn from
+  int more;         // whether a refused draft has younger siblings
 };
 enum { kDone = 0, kRefusal = 1, kDraw = 2 };
 
@@ -48,7 +48,7 @@ struct Args {
   float *top, *row_top, *share;           // [n_tokens][blocks], [n_tokens], [n_tokens]
   int32_t *arg, *above;                   // [n_tokens][blocks], [n_tokens]: parents, -1 where not acceptable
   State* state;                           // [n_seqs]
-  unsigned* arrived;                      // [n_seqs]
+  unsigned* arrived;                      // [n_seqs], kApart of them apart
   int64_t ld, ld_draft;
   int n_seqs, n_tokens, max_new, vocab, type, draft_type;
   int blocks, chunks;                     // of a row: of its statistics, and of a pass
@@ -184,24 +184,36 @@ __global__ void __launch_bounds__(kThreads) stats_kernel(Args a) {
 // a row's probability of a logit, in 64 bits
 __device__ __forceinline__ double prob(double x, float top, double sum, double heat) { return exp((x - top) / heat) / sum; }
 
-// Drafts of a sequence as the walk reads them.
+// Drafts of a sequence as the walk reads them, in LDS that is sized for the call's longest.
+constexpr int kDraftBytes = 32;
 struct Drafts {
-  double prob[kMaxNew];   // at the parent
-  float share[kMaxNew];   // of the draft distribution there
-  float u[kMaxNew];
-  int above[kMaxNew], token[kMaxNew];
-  double sum[kMaxNew];    // of its own row, NaN: no distribution
+  double *prob, *sum;     // at the parent; the sum of its own row, NaN: no distribution
+  float *share, *u;       // of the draft distribution at the parent
+  int *above, *token;
+
+  __device__ __forceinline__ Drafts(char* lds, int most) {
+    prob = reinterpret_cast<double*>(lds);
+    sum = prob + most;
+    share = reinterpret_cast<float*>(sum + most);
+    u = share + most;
+    above = reinterpret_cast<int*>(u + most);
+    token = above + most;
+  }
 };
+
+// the first draft below row `cur` from `from` on, or -1; in one wave
+__device__ __forceinline__ int child(const Drafts& d, int n, int cur, int from, int lane) {
+  for (int j0 = from; j0 < n; j0 += kWave) {
+    const uint64_t kids = __ballot(j0 + lane < n && d.above[j0 + lane] == cur);
+    if (kids) return j0 + __builtin_ctzll(kids);
+  }
+  return -1;
+}
 
 // Walks on, in one wave: to the end, or to a refusal that needs a sum.
 __device__ __forceinline__ void walk(const Args& a, int b, const Seq& s, const Drafts& d, State& st, int lane) {
   for (;;) {
-    // the next draft below cur
-    int i = -1;
-    for (int j0 = st.at + 1; j0 < s.n && i < 0; j0 += kWave) {
-      const uint64_t kids = __ballot(j0 + lane < s.n && d.above[j0 + lane] == st.cur);
-      if (kids) i = j0 + __builtin_ctzll(kids);
-    }
+    const int i = child(d, s.n, st.cur, st.at + 1, lane);
     if (i < 0) {
       st.need = kDraw;
       return;
@@ -240,15 +252,17 @@ __device__ __forceinline__ void walk(const Args& a, int b, const Seq& s, const D
       }
     } else if (a.draft) {
       st.need = kRefusal;
+      st.more = child(d, s.n, st.cur, i + 1, lane) >= 0;
       return;
     }
   }
 }
 
-__global__ void __launch_bounds__(1024) walk_kernel(Args a) {
-  __shared__ Drafts d;
-  __shared__ float tops[kMaxNew];
-  __shared__ int args[kMaxNew];
+__global__ void __launch_bounds__(1024) walk_kernel(Args a, int most) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const Drafts d(lds, most);
+  float* tops = reinterpret_cast<float*>(lds + most * kDraftBytes);
+  int* args = reinterpret_cast<int*>(tops + most);
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, threads = blockDim.x;
   bool ok;
   const Seq s = sequence(a, b, ok);
@@ -317,7 +331,7 @@ __global__ void __launch_bounds__(1024) walk_kernel(Args a) {
     __syncthreads();
   }
   if (tid >= kWave) return;
-  State st{0., 1., 0., 0.f, 0, 0, s.n > 0, kDone};
+  State st{0., 1., 0., 0.f, 0, 0, s.n > 0, kDone, 0};
   if (s.n == 0 || d.sum[0] != d.sum[0]) {
     if (lane == 0) {
       if (s.n) report(a, MOE_ERR_RANGE);
@@ -350,7 +364,7 @@ __global__ void __launch_bounds__(1024) walk_kernel(Args a) {
   if (lane == 0) {
     a.n_keep[b] = st.count;
     a.state[b] = st;
-    a.arrived[b] = 0;
+    a.arrived[static_cast<int64_t>(b) * kApart] = 0;
   }
 }
 
@@ -361,27 +375,29 @@ struct Row {
   double sum, heat, c;
 };
 
-struct Taken {
-  int n, token[kMaxNew];
+struct Taken {   // tokens that were refused, in LDS
+  int* n;
+  int* token;
 };
 
 // a thread's tokens' parts, from `at` on
-__device__ __forceinline__ void parts_of(const Args& a, const Row& r, const Taken& out, int at, double (&v)[kEach]) {
-  float x[kEach], w[kEach];
+template <int EACH>
+__device__ __forceinline__ void parts_of(const Args& a, const Row& r, const Taken& out, int at, double (&v)[EACH]) {
+  float x[EACH], w[EACH];
   load_some(a.type, a.logits, r.row * a.ld + at, a.vocab - at, -INFINITY, x);
   if (r.c > 0.) load_some(a.draft_type, a.draft, r.row * a.ld_draft + at, a.vocab - at, 0.f, w);
   const double inv = 1. / r.heat;
 #pragma unroll
-  for (int e = 0; e < kEach; e++) v[e] = exp((static_cast<double>(x[e]) - r.top) * inv);
+  for (int e = 0; e < EACH; e++) v[e] = exp((static_cast<double>(x[e]) - r.top) * inv);
   if (r.c > 0.) {
     const double scale = 1. / r.sum;
 #pragma unroll
-    for (int e = 0; e < kEach; e++) v[e] = fmax(v[e] * scale - r.c * static_cast<double>(w[e]), 0.);
+    for (int e = 0; e < EACH; e++) v[e] = fmax(v[e] * scale - r.c * static_cast<double>(w[e]), 0.);
   }
-  for (int k = 0; !a.draft && k < out.n; k++) {
+  for (int k = 0; !a.draft && k < *out.n; k++) {
     const int e0 = out.token[k] - at;
 #pragma unroll
-    for (int e = 0; e < kEach; e++) v[e] = e == e0 ? 0. : v[e];
+    for (int e = 0; e < EACH; e++) v[e] = e == e0 ? 0. : v[e];
   }
 }
 
@@ -426,9 +442,12 @@ __device__ __forceinline__ int first_past(double mine, double up, double aim, in
 __device__ __forceinline__ void put_total(double* p, double v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ double read_total(const double* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-__global__ void __launch_bounds__(kThreads) pass_kernel(Args a, int last) {
-  __shared__ Taken taken;
-  __shared__ Drafts d;
+template <int EACH>
+__global__ void __launch_bounds__(kThreads) pass_kernel(Args a, int most, int last) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];   // drafts, or the tokens that are taken out
+  __shared__ int n_taken;
+  const Drafts d(lds, most);
+  const Taken taken{&n_taken, reinterpret_cast<int*>(lds + most * kDraftBytes)};
   __shared__ double parts[kWaves], carry;
   __shared__ int marks[2 * kWaves], chosen;
   __shared__ State shared;
@@ -447,18 +466,18 @@ __global__ void __launch_bounds__(kThreads) pass_kernel(Args a, int last) {
     r.c = a.draft ? st.need == kRefusal ? st.c + st.s : st.c : 0.;
     if (a.draft) return;
     __syncthreads();
-    if (tid == 0) taken.n = 0;
+    if (tid == 0) n_taken = 0;
     __syncthreads();
     if (st.s > 0.)
       for (int j = st.cur + 1 + tid; j < s.n; j += kThreads)
-        if (a.above[s.off + j] == st.cur) taken.token[atomicAdd(&taken.n, 1)] = a.tokens[s.off + j];
+        if (a.above[s.off + j] == st.cur) taken.token[atomicAdd(&n_taken, 1)] = a.tokens[s.off + j];
     __syncthreads();
   };
   auto chunk_sum = [&](int c) {
-    double v[kEach], t = 0.;
-    parts_of(a, r, taken, c * kChunk + tid * kEach, v);
+    double v[EACH], t = 0.;
+    parts_of(a, r, taken, c * (kThreads * EACH) + tid * EACH, v);
 #pragma unroll
-    for (int e = 0; e < kEach; e++) t += v[e];
+    for (int e = 0; e < EACH; e++) t += v[e];
     t = wave_sum64(t);
     __syncthreads();
     if (lane == 0) parts[tid / kWave] = t;
@@ -474,22 +493,14 @@ __global__ void __launch_bounds__(kThreads) pass_kernel(Args a, int last) {
     // arrived, the count may go up.  (A release at device scope writes the whole L2 back, for each
     // workgroup: 64 sequences by 32 chunks 46 us that way.)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    chosen = __hip_atomic_fetch_add(&a.arrived[b], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+    chosen = __hip_atomic_fetch_add(&a.arrived[static_cast<int64_t>(b) * kApart], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
   }
   __syncthreads();
   if (!chosen) return;
   // the last workgroup of the sequence: add up, and walk on
-  if (tid == 0) a.arrived[b] = 0;
-  for (int i = tid; i < s.n; i += kThreads) {
-    d.prob[i] = a.prob[s.off + i];
-    d.share[i] = a.share[s.off + i];
-    d.u[i] = a.u[s.off + i];
-    d.above[i] = a.above[s.off + i];
-    d.token[i] = a.tokens[s.off + i];
-    d.sum[i] = a.row_sum[s.off + i];
-  }
-  __syncthreads();
+  if (tid == 0) a.arrived[static_cast<int64_t>(b) * kApart] = 0;
   const int each = (a.chunks + kThreads - 1) / kThreads;   // chunks of a thread, side by side
+  bool loaded = false;
   for (bool summed = true;;) {
     if (!summed) {   // alone, chunk after chunk
       aim_at();
@@ -504,12 +515,28 @@ __global__ void __launch_bounds__(kThreads) pass_kernel(Args a, int last) {
     const double up = scan(have, parts, tid, all);
     const int need = st.need;
     bool draw = need == kDraw;
-    if (need == kRefusal) {
+    if (need == kRefusal && !st.more && all > 0.) {    // the end: these very sums are drawn from
+      st.c = r.c;
+      st.s = all;
+      draw = true;
+    } else if (need == kRefusal) {
       const int row = st.cur;
+      if (!loaded) {
+        for (int i = tid; i < s.n; i += kThreads) {
+          d.prob[i] = a.prob[s.off + i];
+          d.share[i] = a.share[s.off + i];
+          d.u[i] = a.u[s.off + i];
+          d.above[i] = a.above[s.off + i];
+          d.token[i] = a.tokens[s.off + i];
+          d.sum[i] = a.row_sum[s.off + i];
+        }
+        loaded = true;
+      }
       if (all > 0.) {    // nothing left: as if it had not been refused
         st.c = r.c;
         st.s = all;
       }
+      __syncthreads();
       if (tid < kWave) {
         walk(a, b, s, d, st, lane);
         if (lane == 0) {
@@ -521,8 +548,8 @@ __global__ void __launch_bounds__(kThreads) pass_kernel(Args a, int last) {
       __syncthreads();
       st = shared;
       __syncthreads();
-      draw = st.need == kDraw && st.cur == row && all > 0.;    // these very sums are drawn from
-    } else if (!(all > 0.) && (a.draft ? st.c > 0. : taken.n > 0)) {   // nothing left in 64 bits: the whole row
+      draw = st.need == kDraw && st.cur == row && all > 0.;
+    } else if (!(all > 0.) && (a.draft ? st.c > 0. : n_taken > 0)) {   // nothing left in 64 bits: the whole row
       st.c = 0.;
       st.s = -1.;
       draw = false;
@@ -533,7 +560,8 @@ __global__ void __launch_bounds__(kThreads) pass_kernel(Args a, int last) {
       if (tid == t) {    // the chunk among this thread's
         double before = up - have;
         int at = t * each;
-        for (int c = t * each; c < min((t + 1) * each, a.chunks); c++) {
+        carry = before;
+        for (int c = t * each; each > 1 && c < min((t + 1) * each, a.chunks); c++) {
           const double part = read_total(&total[c]);
           if (part > 0.) {
             at = c;
@@ -545,19 +573,19 @@ __global__ void __launch_bounds__(kThreads) pass_kernel(Args a, int last) {
         chosen = at;
       }
       __syncthreads();
-      const int at = chosen * kChunk + tid * kEach;
+      const int at = chosen * (kThreads * EACH) + tid * EACH;
       const double before = carry;
-      double v[kEach], have2 = 0., all2;
+      double v[EACH], have2 = 0., all2;
       parts_of(a, r, taken, at, v);
 #pragma unroll
-      for (int e = 0; e < kEach; e++) have2 += v[e];
+      for (int e = 0; e < EACH; e++) have2 += v[e];
       const double up2 = before + scan(have2, parts, tid, all2);
       if (tid == first_past(have2, up2, goal, marks, tid)) {
         double sum = up2 - have2;
         int x = 0;
         bool done = false;
 #pragma unroll
-        for (int e = 0; e < kEach; e++) {
+        for (int e = 0; e < EACH; e++) {
           if (!done && v[e] > 0.) x = e;
           sum += v[e];
           done = done || (v[e] > 0. && sum > goal);
@@ -579,6 +607,14 @@ __global__ void __launch_bounds__(kThreads) pass_kernel(Args a, int last) {
 // tokens a thread.
 int each_of(int64_t n_tokens, int64_t vocab) { return n_tokens * cdiv(vocab, 16 * kThreads) > 2048 ? 32 : 16; }
 
+// Tokens of the vocabulary for a thread of a pass: as few (4 to 16, each an exponential in 64
+// bits) as take no more than 1024 workgroups, whose counts at the end would wait for each other.
+int pass_each_of(int64_t n_seqs, int64_t vocab) {
+  int each = 4;
+  while (each < 16 && n_seqs * cdiv(vocab, each * kThreads) > 1024) each *= 2;
+  return each;
+}
+
 struct Layout {
   int64_t blocks, chunks;
   size_t sum, total, row_sum, prob, state, top, row_top, share, arg, above, arrived, bytes;
@@ -586,7 +622,7 @@ struct Layout {
 Layout layout_of(int64_t n_seqs, int64_t n_tokens, int64_t vocab) {
   Layout l;
   l.blocks = cdiv(vocab, each_of(n_tokens, vocab) * kThreads);
-  l.chunks = cdiv(vocab, kChunk);
+  l.chunks = cdiv(vocab, pass_each_of(n_seqs, vocab) * kThreads);
   size_t at = 0;
   auto put = [&](size_t bytes) {
     const size_t here = at;
@@ -603,7 +639,7 @@ Layout layout_of(int64_t n_seqs, int64_t n_tokens, int64_t vocab) {
   l.share = put(4 * n_tokens);
   l.arg = put(4 * n_tokens * l.blocks);
   l.above = put(4 * n_tokens);
-  l.arrived = put(4 * n_seqs);
+  l.arrived = put(4 * n_seqs * kApart);
   l.bytes = at;
   return l;
 }
@@ -710,10 +746,18 @@ extern "C" int moe_draft_verify(const void* logits, int32_t logits_type, int64_t
     else launch_stats<MOE_TYPE_FP16>(wide, most, s, a);
   }
   // a lane for every block of a sequence's rows, if that takes no more than a workgroup
-  hipLaunchKernelGGL(walk_kernel, dim3(n_seqs), dim3(static_cast<int64_t>(most) * a.blocks > kThreads ? 1024 : kThreads), 0, s, a);
+  const int threads = static_cast<int64_t>(most) * a.blocks > kThreads ? 1024 : kThreads;
+  hipLaunchKernelGGL(walk_kernel, dim3(n_seqs), dim3(threads), most * (kDraftBytes + 8), s, a, most);
   if (most > 0 && u) {
-    const int passes = draft && parents ? std::min(kPasses, most) : 1;
-    for (int i = 0; i < passes; i++) hipLaunchKernelGGL(pass_kernel, dim3(a.chunks, n_seqs), block, 0, s, a, i == passes - 1);
+    const int passes = draft && parents ? std::min(kPasses, most) : 1, bytes = most * (kDraftBytes + 4);
+    const int each = pass_each_of(n_seqs, vocab);
+    const dim3 grid(a.chunks, n_seqs);
+    for (int i = 0; i < passes; i++) {
+      const int last = i == passes - 1;
+      if (each == 4) hipLaunchKernelGGL(pass_kernel<4>, grid, block, bytes, s, a, most, last);
+      else if (each == 8) hipLaunchKernelGGL(pass_kernel<8>, grid, block, bytes, s, a, most, last);
+      else hipLaunchKernelGGL(pass_kernel<16>, grid, block, bytes, s, a, most, last);
+    }
   }
   return launch_status(s);
 }
