@@ -137,6 +137,26 @@ def load() -> C.CDLL:
     return L
 
 
+_calls = None
+
+
+def calls():
+    """The module _calls over the loaded library; raises if it is missing (no fallback path)."""
+    global _calls
+    if _calls is None:
+        L = load()
+        try:
+            from . import _calls as mod
+        except ImportError as e:
+            raise MoEError("_calls.so is not built (run __graft_entry__.build() or "
+                           "python paper_2503_21135_amd/build.py): %s" % e) from e
+        names = ("moe_cache_append_norm", "moe_qcache_append", "moe_qcache_read", "moe_qcache_attention",
+                 "moe_qcache_keep", "moe_draft_verify")
+        mod.bind(MoEError, *(C.cast(getattr(L, n), C.c_void_p).value for n in names))
+        _calls = mod
+    return _calls
+
+
 def stream_capturing(handle: int) -> bool:
     """Whether a graph is being captured on the stream (asked of the HIP runtime that the
     library is linked to; making the stream current to ask torch takes 6 us)."""

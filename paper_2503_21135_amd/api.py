@@ -14,7 +14,7 @@ from typing import Optional, Tuple
 import numpy as np
 import torch
 
-from ._lib import (TYPE_BF16, TYPE_FP16, TYPE_FP32, CacheDesc, LayerDesc, MoEError, QuantCacheDesc, check, load,
+from ._lib import (TYPE_BF16, TYPE_FP16, TYPE_FP32, CacheDesc, LayerDesc, MoEError, QuantCacheDesc, calls, check, load,
                    stream_capturing)
 
 
@@ -393,71 +393,28 @@ def moe_cache_keep(desc: CacheDesc, table: torch.Tensor, lens: torch.Tensor, new
 # ---------------------------------------------------------------------------
 # normed heads, the cache in 8 bits, verification of drafts
 # ---------------------------------------------------------------------------
-def _run(name: str, dev: int, *args) -> None:
-    """Calls an entry point with device `dev`, where its tensors are, current."""
+# These take tensors to the entry points by way of the module _calls, which checks them (types,
+# shapes, strides, one device) in a tenth of the time that it takes here.
+def _native(what: str, at: torch.Tensor, call: str, stream, *args) -> None:
+    """Makes a call of _calls with the device that `at` is on current, and its stream."""
+    dev = at.get_device()
+    if dev < 0:
+        raise MoEError("%s: expected device tensors" % what)
+    args = (*args, torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream)
     if dev == torch._C._cuda_getDevice():
-        st = getattr(load(), name)(*args)
+        st = getattr(calls(), call)(*args)
     else:
         with torch.cuda.device(dev):
-            st = getattr(load(), name)(*args)
+            st = getattr(calls(), call)(*args)
     if st:
-        check(st, name)
+        check(st, what)
 
 
-def _on(t: torch.Tensor, what: str) -> int:
-    """The device that a call works on: where `t` is, and its other tensors have to be."""
-    dev = t.get_device()
-    if dev < 0:
-        raise MoEError("%s must be a device tensor" % what)
-    return dev
-
-
-def _array(t: Optional[torch.Tensor], n: int, dtype: torch.dtype, dev: int, what: str):
-    """Data pointer of a contiguous array of n values on device `dev` (None for None)."""
-    if t is None:
-        return None
-    if t.dtype is dtype and t.numel() == n and t.get_device() == dev and t.is_contiguous():
-        return t.data_ptr()
-    raise MoEError("%s must be %d contiguous values of %s on device %d, not %s of %s on %s"
-                   % (what, n, dtype, dev, tuple(t.shape), t.dtype, t.device))
-
-
-def _heads_on(t: torch.Tensor, N: int, H: int, D: int, dtype: torch.dtype, dev: int, what: str) -> Tuple[int, int]:
-    """_heads on device `dev`."""
-    if t.dtype is dtype and t.get_device() == dev and t.shape == (N, H, D):
-        s = t.stride()
-        if s[2] == 1 and (s[1] == D or H <= 1):
-            return t.data_ptr(), s[0] if N > 1 else H * D
-    raise MoEError("%s must be a %s tensor of shape (%d, %d, %d) on device %d, the heads of a token side by side"
-                   % (what, dtype, N, H, D, dev))
-
-
-def _batch_on(table: torch.Tensor, lens: torch.Tensor, new_off: torch.Tensor, dev: int):
-    """_batch on device `dev`."""
-    B, (rows, pages) = lens.numel(), table.shape
-    return (_array(table, B * pages, torch.int32, dev, "table"), pages, _array(lens, B, torch.int32, dev, "cache_len"), B,
-            _array(new_off, B + 1, torch.int32, dev, "new_off"))
-
-
-def _append(name, desc, table, lens, new_off, max_new, q, k, v, q_out, w_q, w_k, eps, positions, cos, sin, interleaved,
-            status, stream) -> None:
-    dev, dt, D, Hkv = _on(k, "k"), _DTYPE16[desc.type], desc.head_dim, desc.n_heads
-    N = k.shape[0]
-    if (q is None) != (q_out is None) or (cos is None) != (sin is None):
-        raise MoEError("q and q_out, cos and sin come in pairs")
-    rows, half = (1, 0) if cos is None else cos.shape
-    qp, ld_q, Hq, op, ld_o = None, 0, 0, None, 0
-    f32, i32 = torch.float32, torch.int32
-    if q is not None:
-        Hq = q.shape[1]
-        qp, ld_q = _heads_on(q, N, Hq, D, dt, dev, "q")
-        op, ld_o = _heads_on(q_out, N, Hq, D, dt, dev, "q_out")
-    kp, ld_k = _heads_on(k, N, Hkv, D, dt, dev, "k")
-    vp, ld_v = _heads_on(v, N, Hkv, D, dt, dev, "v")
-    _run(name, dev, C.byref(desc), *_batch_on(table, lens, new_off, dev), N, max_new, qp, ld_q, Hq, kp, ld_k, vp, ld_v,
-         _array(w_q, D, f32, dev, "w_q"), _array(w_k, D, f32, dev, "w_k"), eps, _array(positions, N, i32, dev, "positions"),
-         _array(cos, rows * half, f32, dev, "cos"), _array(sin, rows * half, f32, dev, "sin"), 2 * half, rows,
-         int(interleaved), op, ld_o, _array(status, 1, i32, dev, "status"), _stream(stream, k))
+def _at(desc, kind) -> int:
+    """Address of a cache's description."""
+    if type(desc) is not kind:
+        raise MoEError("expected the description of another kind of cache: %s" % kind.__name__)
+    return C.addressof(desc)
 
 
 def moe_cache_append_norm(desc: CacheDesc, table: torch.Tensor, lens: torch.Tensor, new_off: torch.Tensor,
@@ -468,8 +425,8 @@ def moe_cache_append_norm(desc: CacheDesc, table: torch.Tensor, lens: torch.Tens
                           interleaved: bool = False, status: Optional[torch.Tensor] = None, stream=None) -> None:
     """moe_cache_append with a norm of each head (weights w_q, w_k float32 [head_dim], None:
     none) before the rotation."""
-    _append("moe_cache_append_norm", desc, table, lens, new_off, max_new, q, k, v, q_out, w_q, w_k, eps, positions, cos,
-            sin, interleaved, status, stream)
+    _native("moe_cache_append_norm", k, "append_norm", stream, _at(desc, CacheDesc), table, lens, new_off, max_new, q,
+            k, v, q_out, w_q, w_k, eps, positions, cos, sin, interleaved, status)
 
 
 def moe_qcache_append(desc: QuantCacheDesc, table: torch.Tensor, lens: torch.Tensor, new_off: torch.Tensor,
@@ -480,8 +437,8 @@ def moe_qcache_append(desc: QuantCacheDesc, table: torch.Tensor, lens: torch.Ten
                       sin: Optional[torch.Tensor] = None, interleaved: bool = False,
                       status: Optional[torch.Tensor] = None, stream=None) -> None:
     """moe_cache_append_norm into a cache in 8 bits."""
-    _append("moe_qcache_append", desc, table, lens, new_off, max_new, q, k, v, q_out, w_q, w_k, eps, positions, cos, sin,
-            interleaved, status, stream)
+    _native("moe_qcache_append", k, "append", stream, _at(desc, QuantCacheDesc), table, lens, new_off, max_new, q, k, v,
+            q_out, w_q, w_k, eps, positions, cos, sin, interleaved, status)
 
 
 def moe_qcache_read(desc: QuantCacheDesc, table: torch.Tensor, first: torch.Tensor, row_off: torch.Tensor, max_rows: int,
@@ -492,12 +449,8 @@ def moe_qcache_read(desc: QuantCacheDesc, table: torch.Tensor, first: torch.Tens
     at = k_out if k_out is not None else v_out
     if at is None:
         raise MoEError("k_out or v_out must be given")
-    dev, dt, D, H = _on(at, "k_out, v_out"), _DTYPE16[desc.type], desc.head_dim, desc.n_heads
-    N = at.shape[0]
-    kp, ld_k = (None, 0) if k_out is None else _heads_on(k_out, N, H, D, dt, dev, "k_out")
-    vp, ld_v = (None, 0) if v_out is None else _heads_on(v_out, N, H, D, dt, dev, "v_out")
-    _run("moe_qcache_read", dev, C.byref(desc), *_batch_on(table, first, row_off, dev), N, max_rows, kp, ld_k, vp, ld_v,
-         _array(status, 1, torch.int32, dev, "status"), _stream(stream, at))
+    _native("moe_qcache_read", at, "read", stream, _at(desc, QuantCacheDesc), table, first, row_off, max_rows, k_out, v_out,
+            status)
 
 
 def moe_qcache_attention_plan(desc: QuantCacheDesc, n_q_heads: int, n_seqs: int, max_new: int,
@@ -514,26 +467,16 @@ def moe_qcache_attention(desc: QuantCacheDesc, table: torch.Tensor, lens: torch.
                          mask: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
                          status: Optional[torch.Tensor] = None, stream=None) -> None:
     """moe_tree_attention over a cache in 8 bits."""
-    dev, dt, (N, Hq, D) = _on(q, "q"), _DTYPE16[desc.type], q.shape
-    if D != desc.head_dim:
-        raise MoEError("q has heads of %d, the cache of %d" % (D, desc.head_dim))
-    words = 0 if mask is None else mask.shape[-1]
-    qp, ld_q = _heads_on(q, N, Hq, D, dt, dev, "q")
-    op, ld_o = _heads_on(out, N, Hq, D, dt, dev, "out")
-    wb = 0 if ws is None else ws.numel()
-    _run("moe_qcache_attention", dev, C.byref(desc), *_batch_on(table, lens, new_off, dev), N, max_new, max_len, qp, ld_q,
-         Hq, _array(mask, N * words, torch.int64, dev, "mask"), words, scale, op, ld_o,
-         _array(status, 1, torch.int32, dev, "status"), _array(ws, wb, torch.uint8, dev, "ws"), wb, _stream(stream, q))
+    _native("moe_qcache_attention", q, "attention", stream, _at(desc, QuantCacheDesc), table, lens, new_off, max_new,
+            max_len, q, out, scale, mask, ws, status)
 
 
 def moe_qcache_keep(desc: QuantCacheDesc, table: torch.Tensor, lens: torch.Tensor, new_off: torch.Tensor,
                     keep: torch.Tensor, n_keep: torch.Tensor, len_out: Optional[torch.Tensor] = None,
                     status: Optional[torch.Tensor] = None, stream=None) -> None:
     """moe_cache_keep for a cache in 8 bits."""
-    dev, B, wide, i32 = _on(lens, "cache_len"), lens.numel(), keep.shape[-1], torch.int32
-    _run("moe_qcache_keep", dev, C.byref(desc), *_batch_on(table, lens, new_off, dev), _array(keep, B * wide, i32, dev, "keep"),
-         wide, _array(n_keep, B, i32, dev, "n_keep"), _array(len_out, B, i32, dev, "len_out"),
-         _array(status, 1, i32, dev, "status"), _stream(stream, lens))
+    _native("moe_qcache_keep", lens, "keep", stream, _at(desc, QuantCacheDesc), table, lens, new_off, keep, n_keep, len_out,
+            status)
 
 
 def moe_draft_verify_plan(n_seqs: int, n_tokens: int, max_new: int, vocab: int) -> int:
@@ -551,20 +494,8 @@ def moe_draft_verify(logits: torch.Tensor, tokens: torch.Tensor, new_off: torch.
                      stream=None) -> None:
     """Which of the drafts tokens [tokens] the logits [tokens][vocab] accept, and the token after
     them: keep [sequences][max_new], n_keep and next_token [sequences], all int32."""
-    dev, (N, V), B = _on(logits, "logits"), logits.shape, n_keep.numel()
-    lp, ld = _rows(logits, N, V, "logits")
-    dp, ld_d, d_type = None, 0, 0
-    if draft_probs is not None:
-        (dp, ld_d), d_type = _rows(draft_probs, N, V, "draft_probs"), _type(draft_probs, "draft_probs")
-        if draft_probs.get_device() != dev:
-            raise MoEError("draft_probs must be on device %d" % dev)
-    i32, f32, wb = torch.int32, torch.float32, ws.numel()
-    _run("moe_draft_verify", dev, lp, _type(logits, "logits"), ld, N, V, _array(tokens, N, i32, dev, "tokens"),
-         _array(parents, N, i32, dev, "parents"), _array(new_off, B + 1, i32, dev, "new_off"), B, max_new, dp, d_type, ld_d,
-         _array(temperature, B, f32, dev, "temperature"), _array(u, N, f32, dev, "u"), _array(u_next, B, f32, dev, "u_next"),
-         _array(keep, B * max_new, i32, dev, "keep"), _array(n_keep, B, i32, dev, "n_keep"),
-         _array(next_token, B, i32, dev, "next_token"), _array(status, 1, i32, dev, "status"),
-         _array(ws, wb, torch.uint8, dev, "ws"), wb, _stream(stream, logits))
+    _native("moe_draft_verify", logits, "verify", stream, logits, tokens, new_off, max_new, keep, n_keep, next_token,
+            ws, parents, draft_probs, u, u_next, temperature, status)
 
 
 # ---------------------------------------------------------------------------

@@ -155,8 +155,8 @@ class PagedCache:
             api.moe_cache_append(self.desc, self.table, self.lens, new_off, max_new, q, k, v, q_out, positions, cos,
                                  sin, interleaved, self.status, stream)
         else:
-            api._append("moe_cache_append_norm", self.desc, self.table, self.lens, new_off, max_new, q, k, v, q_out, w_q,
-                        w_k, eps, positions, cos, sin, interleaved, self.status, stream)
+            api.moe_cache_append_norm(self.desc, self.table, self.lens, new_off, max_new, q, k, v, q_out, w_q, w_k, eps,
+                                      positions, cos, sin, interleaved, self.status, stream)
 
     # the entry points of this kind of cache
     def _plan(self, *sizes) -> int:
@@ -247,8 +247,8 @@ class QuantPagedCache(PagedCache):
         return cls(k, v, ks, vs, table, torch.zeros(n_seqs, dtype=torch.int32, device=device), dtype)
 
     def _append(self, new_off, max_new, q, k, v, q_out, w_q, w_k, eps, positions, cos, sin, interleaved, stream) -> None:
-        api._append("moe_qcache_append", self.desc, self.table, self.lens, new_off, max_new, q, k, v, q_out, w_q, w_k, eps,
-                    positions, cos, sin, interleaved, self.status, stream)
+        api.moe_qcache_append(self.desc, self.table, self.lens, new_off, max_new, q, k, v, q_out, w_q, w_k, eps,
+                              positions, cos, sin, interleaved, self.status, stream)
 
     def _plan(self, *sizes) -> int:
         return api.moe_qcache_attention_plan(self.desc, *sizes)[1]

@@ -1,4 +1,5 @@
-"""Build the gfx950 kernel library libmoe_quant.so in-tree with hipcc."""
+"""Build the gfx950 kernel library libmoe_quant.so in-tree with hipcc, and the Python module
+_calls that marshals tensors into it with the host compiler."""
 from __future__ import annotations
 
 import glob
@@ -9,7 +10,9 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libmoe_quant.so")
+CALLS = os.path.join(HERE, "_calls.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+CXX = os.environ.get("CXX", "g++")
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -36,12 +39,29 @@ def _run(cmd, verbose):
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         sys.stderr.write(res.stdout + res.stderr)
-        raise RuntimeError("hipcc failed: %s" % " ".join(cmd))
+        raise RuntimeError("%s failed: %s" % (os.path.basename(cmd[0]), " ".join(cmd)))
+
+
+def build_calls(verbose: bool = False) -> str:
+    """Compile csrc/calls.cc into paper_2503_21135_amd/_calls.so, against the installed torch."""
+    import sysconfig
+
+    import torch
+    root = os.path.join(os.path.dirname(torch.__file__))
+    tmp = CALLS + ".tmp%d" % os.getpid()
+    _run([CXX, "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Wno-unused-function",
+          "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
+          "-I", os.path.join(ROOT, "include"), "-isystem", os.path.join(root, "include"),
+          "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
+          "-isystem", sysconfig.get_paths()["include"], os.path.join(HERE, "csrc", "calls.cc"), "-o", tmp,
+          "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"], verbose)
+    os.replace(tmp, CALLS)
+    return CALLS
 
 
 def build(verbose: bool = False) -> str:
-    """Compile every HIP source into paper_2503_21135_amd/libmoe_quant.so:
-    one object per source, compiled in parallel, then one link."""
+    """Compile every HIP source into paper_2503_21135_amd/libmoe_quant.so: one object per
+    source, compiled in parallel, then one link; and the module _calls beside them."""
     from concurrent.futures import ThreadPoolExecutor
     obj_dir = os.path.join(ROOT, "_build", "obj%d" % os.getpid())
     os.makedirs(obj_dir, exist_ok=True)
@@ -56,8 +76,10 @@ def build(verbose: bool = False) -> str:
     objs = [os.path.join(obj_dir, "%d_%s.o" % (i, os.path.basename(u[0]))) for i, u in enumerate(units)]
     jobs = max(1, min(len(units), int(os.environ.get("MAX_JOBS", os.cpu_count() or 1))))
     with ThreadPoolExecutor(jobs) as ex:
+        calls = ex.submit(build_calls, verbose)
         list(ex.map(lambda uo: _run([HIPCC] + FLAGS + uo[0][1] + ["-c"] + inc + [uo[0][0], "-o", uo[1]],
                                     verbose), zip(units, objs)))
+        calls.result()
     tmp = LIB + ".tmp%d" % os.getpid()
     _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC"] + objs + ["-o", tmp], verbose)
     os.replace(tmp, LIB)

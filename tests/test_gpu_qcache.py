@@ -608,3 +608,39 @@ def test_block_over_a_cache_in_8_bits():
         results.append(tree_r)
     # a code is off by 2^-8 of a row's largest value at most: less than a hundredth in norm, twice
     assert ((results[0] - results[1]).norm() / results[1].norm()).item() < 2e-2
+
+
+def test_tensors_that_do_not_fit_are_refused():
+    """Types, shapes, strides and devices, before any device work: nothing is written."""
+    pkg = P()
+    cache, off = qbatch([10, 20], [2, 3], 64, 2, 64, BF16, 4)
+    was = cache.k.clone(), cache.v.clone(), cache.k_scale.clone(), cache.v_scale.clone()
+    kv = torch.randn(5, 2, 64, device="cuda").to(BF16)
+    q, w, tab = torch.randn(5, 4, 64, device="cuda").to(BF16), torch.ones(64, device="cuda"), torch.ones(50, 32, device="cuda")
+    pos = torch.arange(5, device="cuda").int()
+    ok = dict(q=q, k=kv, v=kv, new_off=off, max_new=3, positions=pos, cos=tab, sin=tab, w_q=w, w_k=w)
+    wide = torch.randn(5, 4, 128, device="cuda").to(BF16)
+    for bad in (dict(k=kv.half()), dict(k=kv[:, :1]), dict(k=kv.cpu()), dict(v=kv[:4]), dict(q=wide[..., ::2]), dict(q=q.float()),
+                dict(q=q.transpose(0, 1)), dict(q=q.cpu()), dict(w_q=w[:32]), dict(w_k=w.half()), dict(w_k=w.cpu()),
+                dict(positions=pos.long()), dict(positions=pos[:4]), dict(cos=None), dict(sin=tab[:40]), dict(cos=tab.t()),
+                dict(new_off=off[:2]), dict(new_off=off.long()), dict(q_out=q[:, :2]), dict(max_new=1 << 40), dict(k=None)):
+        with pytest.raises((pkg.MoEError, AttributeError, TypeError)):
+            cache.append(**dict(ok, **bad))
+    with pytest.raises(pkg.MoEError):
+        pkg.moe_cache_append_norm(cache.desc, cache.table, cache.lens, off, 3, q, kv, kv, q, w, w)   # another kind of cache
+    mask = torch.zeros(5, 1, dtype=torch.int64, device="cuda")
+    for bad in (dict(q=q.half()), dict(q=wide), dict(mask=mask.int()), dict(mask=mask[:3]), dict(out=q[:, :3]), dict(scale=math.inf),
+                dict(new_off=off.cpu()), dict(q=wide[..., 1:65])):
+        with pytest.raises(pkg.MoEError):
+            cache.attend(**dict(dict(q=q, new_off=off, max_new=3, max_len=23), **bad))
+    for bad in (dict(k_out=kv[:, :1]), dict(k_out=kv.half()), dict(first=cache.lens.long()), dict(row_off=off[:2]), dict(v_out=kv)):
+        with pytest.raises(pkg.MoEError):
+            cache.read(**dict(dict(first=cache.lens, row_off=off, max_rows=3, k_out=kv), **bad))
+    with pytest.raises(pkg.MoEError):
+        cache.read(cache.lens, off, 3)
+    keep, n = torch.zeros(2, 2, dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    for bad in (dict(keep=keep.long()), dict(keep=keep.t()), dict(n_keep=n[:1]), dict(len_out=cache.lens), dict(len_out=n)):
+        with pytest.raises(pkg.MoEError):
+            cache.keep(**dict(dict(new_off=off, keep=keep if "keep" not in bad else None, n_keep=n), **bad))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(was, (cache.k, cache.v, cache.k_scale, cache.v_scale)))

@@ -326,3 +326,20 @@ def test_kept_drafts_go_to_the_cache():
     got, _ = cache.read(cache.lens, ends, 6, rows=int(ends[-1]))
     rows = [s["off"][b] + k for b, ks in enumerate(keep.tolist()) for k in ks if k >= 0]
     assert torch.equal(got, all_k[rows])
+
+
+def test_tensors_that_do_not_fit_are_refused():
+    pkg = P()
+    s = drafts([3, 4], 50, "tree", 3, FP32, FP32)
+    ok = dict(logits=s["logits"], tokens=s["tokens"], new_off=i32(s["off"]), max_new=4, parents=i32(s["parents"]),
+              draft_probs=s["draft"], u=s["u"], u_next=s["last"], temperature=torch.ones(2, device="cuda"))
+    v = pkg.DraftVerifier()
+    v(**ok)
+    for bad in (dict(logits=s["logits"].double()), dict(logits=s["logits"].t().contiguous().t()), dict(tokens=s["tokens"].long()),
+                dict(tokens=s["tokens"][:5]), dict(new_off=ok["new_off"].long()), dict(parents=ok["parents"][:3]),
+                dict(draft_probs=s["draft"][:, :40]), dict(draft_probs=s["draft"].double()), dict(u=None), dict(u_next=None),
+                dict(u=s["u"].half()), dict(u_next=s["last"][:1]), dict(temperature=torch.ones(3, device="cuda")),
+                dict(tokens=s["tokens"].cpu()), dict(draft_probs=s["draft"].cpu()), dict(max_new=2000)):
+        with pytest.raises(pkg.MoEError):
+            v(**dict(ok, **bad))
+    assert v.status_value() == 0
