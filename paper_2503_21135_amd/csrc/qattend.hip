@@ -134,19 +134,18 @@ struct Rows16 {
       ms[rt] = m2 == -INFINITY ? -INFINITY : ms2;
     }
   }
-  template <bool EDGE, class V>
-  __device__ __forceinline__ void weights(int rt, const f32x4 (&sc)[4], V inverses, uint32_t see, u32x4 (&pf)[2]) {
+  template <bool EDGE, bool REST, class V>
+  __device__ __forceinline__ void weights(int rt, const f32x4 (&sc)[4], V inverses, uint32_t see, u32x4 (&pf)[2], u32x4 (&rest)[2]) {
     const float by = ms[rt] == -INFINITY ? 0.f : ms[rt];
-    // Cut to fp16's bits in fp32 first: their sum takes the cut weights, so that the cut of one
-    // that outweighs the rest cancels, and still has those whose value scale is so small that
-    // the product is below fp16's range (a row of zeros takes its share of the softmax).
 #pragma unroll
     for (int kt = 0; kt < 4; kt++) {
       const f32x4 rv = inverses(kt);
       float p[4];
 #pragma unroll
       for (int i = 0; i < 4; i++) {
-        p[i] = __uint_as_float(__float_as_uint(__builtin_amdgcn_exp2f(sc[kt][i] - by)) & 0xFFFFE000u);
+        p[i] = __builtin_amdgcn_exp2f(sc[kt][i] - by);
+        // the sum's terms stay fp32: of a row of values so small that the product is below fp16's
+        // range, of zeros for one, it still takes the share of the softmax
         float r = __fmaf_rn(p[i], rv[i], l[rt]);
         if constexpr (EDGE) {
           p[i] = see >> (4 * kt + i) & 1 ? p[i] : 0.f;
@@ -154,8 +153,12 @@ struct Rows16 {
         }
         l[rt] = r;
       }
-      pf[kt >> 1][kt % 2 * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(p[0], p[1]));
-      pf[kt >> 1][kt % 2 * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(p[2], p[3]));
+#pragma unroll
+      for (int i = 0; i < 4; i += 2) {
+        const uint32_t w = pack2<MOE_TYPE_FP16>(p[i], p[i + 1]);
+        pf[kt >> 1][kt % 2 * 2 + i / 2] = w;
+        if constexpr (REST) rest[kt >> 1][kt % 2 * 2 + i / 2] = pack2<MOE_TYPE_FP16>(p[i] - half_lo<MOE_TYPE_FP16>(w), p[i + 1] - half_hi<MOE_TYPE_FP16>(w));
+      }
     }
   }
 };
@@ -189,6 +192,9 @@ __global__ void __launch_bounds__(64 * RW * KW, RW * KW == 8 || (RW == 1 && D <=
     Sums sums;
   };
   constexpr bool kShared = RW > 1, kAhead = RT * D <= 128;
+  // Weights are rounded to fp16.  Few rows with fp16 outputs, which wait for HBM, add the product
+  // with what the rounding left over.
+  constexpr bool kRest = !kShared && TYPE == MOE_TYPE_FP16;
   __shared__ __attribute__((aligned(16))) char lds_bytes[kShared ? (KW > 1 ? sizeof(Lds) : sizeof(Tile) * 2) : sizeof(Sums)];
   __shared__ float stats[W][RT][16][2];
   // row blocks of a unit (sequence, head, part) sit 8 workgroups apart, on one XCD, and
@@ -277,12 +283,12 @@ __global__ void __launch_bounds__(64 * RW * KW, RW * KW == 8 || (RW == 1 && D <=
           for (int rt = 0; rt < RT; rt++) sc[rt][kt] = product<TYPE>(k, qf[rt][c], c ? sc[rt][kt] : f32x4{0.f, 0.f, 0.f, 0.f});
         }
       }
-      u32x4 pf[RT][2];
+      u32x4 pf[RT][2], rest[RT][2];
       const float k2 = ks * a.scale2, lg = __builtin_amdgcn_logf(vs), rv = __builtin_amdgcn_rcpf(vs);
 #pragma unroll
       for (int rt = 0; rt < RT; rt++) {
         st.template exponents<EDGE>(rt, sc[rt], [&](int kt) { return from_lanes(k2, kt); }, [&](int kt) { return from_lanes(lg, kt); }, see[rt]);
-        st.template weights<EDGE>(rt, sc[rt], [&](int kt) { return from_lanes(rv, kt); }, see[rt], pf[rt]);
+        st.template weights<EDGE, kRest>(rt, sc[rt], [&](int kt) { return from_lanes(rv, kt); }, see[rt], pf[rt], rest[rt]);
       }
 #pragma unroll
       for (int v = 0; v < NV; v++)
@@ -290,7 +296,10 @@ __global__ void __launch_bounds__(64 * RW * KW, RW * KW == 8 || (RW == 1 && D <=
         for (int e = 0; e < 2; e++) {
           const u32x4 w = operand<MOE_TYPE_FP16>(vf[v], e);
 #pragma unroll
-          for (int rt = 0; rt < RT; rt++) st.o[rt][v] = product<MOE_TYPE_FP16>(w, pf[rt][e], st.o[rt][v]);
+          for (int rt = 0; rt < RT; rt++) {
+            st.o[rt][v] = product<MOE_TYPE_FP16>(w, pf[rt][e], st.o[rt][v]);
+            if constexpr (kRest) st.o[rt][v] = product<MOE_TYPE_FP16>(w, rest[rt][e], st.o[rt][v]);
+          }
         }
     };
     // the next tile's keys load behind this one's products; tiles with drafts in them, the
@@ -403,7 +412,7 @@ __global__ void __launch_bounds__(64 * RW * KW, RW * KW == 8 || (RW == 1 && D <=
       for (int rt = 0; rt < RT; rt++)
         st.template exponents<EDGE>(rt, sc[rt], [&](int kt) { return tile.k2[4 * grp + kt]; }, [&](int kt) { return tile.lg[4 * grp + kt]; }, see[rt]);
 #pragma unroll
-      for (int rt = 0; rt < RT; rt++) st.template weights<EDGE>(rt, sc[rt], [&](int kt) { return tile.rv[4 * grp + kt]; }, see[rt], pf[rt]);
+      for (int rt = 0; rt < RT; rt++) st.template weights<EDGE, false>(rt, sc[rt], [&](int kt) { return tile.rv[4 * grp + kt]; }, see[rt], pf[rt], pf[rt]);
 #pragma unroll
       for (int v = 0; v < NV; v++)
 #pragma unroll

@@ -248,9 +248,9 @@ def test_read(lens, new, page, Hkv, D, dt):
 def attention_want(cache, lens, new, q, sees, scale, dt):
     """The definition in 64 bits over the values the rows stand for, and its bound.  Scores are off
     by (D + 8) E32 of their absolute sums (e, times scale), and by the rounding of an exponent
-    of up to 2^8 (2^-16); a weight is cut to fp16's 11 bits in both sums (2^-10 of it in each),
-    or, where weight times value scale is 2^-12 of the row's largest or less, may be off by 2^-22 of
-    that largest; sums by (keys / 16 + 64) E32."""
+    of up to 2^8 (2^-16); a weight is rounded to fp16 in the values' sum (U[FP16]), or, where weight
+    times value scale is 2^-12 of the row's largest or less, may be off by 2^-22 of that largest;
+    sums by (keys / 16 + 64) E32."""
     outs, bounds, n0 = [], [], 0
     Hq, D = q.shape[1], q.shape[2]
     for b in range(len(lens)):
@@ -274,7 +274,7 @@ def attention_want(cache, lens, new, q, sees, scale, dt):
             o, mag = torch.matmul(w, vv), torch.matmul(w, vv.abs())
             most = (w * s).amax(2, keepdim=True)
             lost = torch.minimum(most * 2.0 ** -22, w * s) * (w * s < most * 2.0 ** -12)
-            rel = 4 * e + 2.0 ** -15 + 4 * U[FP16] + (len(see) / 16 + 64) * E32
+            rel = 4 * e + 2.0 ** -15 + 1.01 * U[FP16] + (len(see) / 16 + 64) * E32
             bd = rel * mag + torch.matmul(lost, vc[see].abs().transpose(0, 1).contiguous())
             outs.append(o.reshape(Hq, D))
             bounds.append((bd + U[dt] * 1.01 * (o.abs() + bd) + TINY[dt]).reshape(Hq, D))
