@@ -12,7 +12,7 @@
 //                  to the first sum that it needs
 //   pass_kernel    per sequence and chunk: that sum; the last workgroup of a sequence adds up and
 //                  walks on, and at the end of the walk draws.  Launched once for chains and picked
-//                  drafts, kPasses times for drawn trees; the last launch sees to the rest alone.
+//                  drafts, a few times for drawn trees; the last launch sees to the rest alone.
 #include <algorithm>
 
 #include "elem.hpp"
@@ -24,7 +24,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kMaxNew = 1024;
-constexpr int kPasses = 4;
 constexpr int kApart = 32;          // counters to a cache line of their own: the card takes one count a line at a time
 
 // Where a sequence's walk stands.
@@ -502,11 +501,19 @@ __global__ void __launch_bounds__(kThreads) pass_kernel(Args a, int most, int la
   const int each = (a.chunks + kThreads - 1) / kThreads;   // chunks of a thread, side by side
   bool loaded = false;
   for (bool summed = true;;) {
-    if (!summed) {   // alone, chunk after chunk
+    if (!summed) {   // alone, a chunk to a wave
       aim_at();
-      for (int c = 0; c < a.chunks; c++) {
-        const double t = chunk_sum(c);
-        if (tid == 0) put_total(&total[c], t);
+      for (int c = tid / kWave; c < a.chunks; c += kWaves) {
+        double t = 0.;
+#pragma unroll 1
+        for (int i = 0; i < kWaves; i++) {
+          double v[EACH];
+          parts_of(a, r, taken, c * (kThreads * EACH) + (i * kWave + lane) * EACH, v);
+#pragma unroll
+          for (int e = 0; e < EACH; e++) t += v[e];
+        }
+        t = wave_sum64(t);
+        if (lane == 0) put_total(&total[c], t);
       }
       __syncthreads();
     }
@@ -749,7 +756,11 @@ extern "C" int moe_draft_verify(const void* logits, int32_t logits_type, int64_t
   const int threads = static_cast<int64_t>(most) * a.blocks > kThreads ? 1024 : kThreads;
   hipLaunchKernelGGL(walk_kernel, dim3(n_seqs), dim3(threads), most * (kDraftBytes + 8), s, a, most);
   if (most > 0 && u) {
-    const int passes = draft && parents ? std::min(kPasses, most) : 1, bytes = most * (kDraftBytes + 4);
+    // A drawn tree takes a pass for each refusal of its walk.  What the launches leave is summed by one
+    // workgroup (0.7 us a chunk); one with nothing to do takes 2 us.  16 trees of 31 over 131072 tokens:
+    // 80 us with 4, 85 with 6, or, where a walk refuses 5 times, 127 with 4, 93 with 6.
+    const int passes = draft && parents ? std::min(most, a.chunks == 1 ? 1 : a.chunks <= 4 ? 3 : a.chunks <= 32 ? 4 : 6) : 1;
+    const int bytes = most * (kDraftBytes + 4);
     const int each = pass_each_of(n_seqs, vocab);
     const dim3 grid(a.chunks, n_seqs);
     for (int i = 0; i < passes; i++) {
