@@ -2,9 +2,9 @@
 
 A small model (random weights): embedding, two DecoderBlocks (4-bit projections, paged
 cache, tree attention, mixed-precision MoE layer) and a 4-bit vocabulary projection.
-Each step drafts a tree of tokens, runs the whole tree through the model at once, follows
-the greedy choices down the tree, keeps the accepted path in every layer's cache and
-drafts again from there.
+Each step drafts a tree of tokens, runs the whole tree through the model at once, has the
+drafts verified against its logits, keeps the accepted path in every layer's cache and
+drafts again from there.  Greedily, or with random numbers; over caches of 16 or 8 bits.
 
     python examples/draft_decode.py
 """
@@ -22,7 +22,7 @@ import paper_2503_21135_amd as P  # noqa: E402
 
 
 class Model:
-    def __init__(self, n_blocks=2, vocab=500, heads=(4, 2, 64), max_len=512, seed=0):
+    def __init__(self, n_blocks=2, vocab=500, heads=(4, 2, 64), max_len=512, seed=0, cache=P.PagedCache, page=32, norms=False):
         dev = "cuda:0"
         g = torch.Generator(device=dev).manual_seed(seed)
         layer = mi.WORKLOADS["tiny"].layer
@@ -30,13 +30,15 @@ class Model:
 
         def w(*shape, scale=0.06):
             return scale * torch.randn(*shape, device=dev, generator=g)
+        def head_norms():   # of each query and key head, where the model has them
+            return dict(q=1 + w(D), k=1 + w(D)) if norms else {}
         angle = torch.arange(max_len, device=dev)[:, None] * 10000.0 ** (-torch.arange(D // 2, device=dev) / (D // 2))
         self.blocks = [P.DecoderBlock(P.MoELayer(mi.LayerInputs(layer), device=dev), w((Hq + 2 * Hkv) * D, d), w(d, Hq * D),
-                                      Hq, Hkv, D, dict(attn=1 + w(d), ffn=1 + w(d), attn_post=1 + w(d), ffn_post=1 + w(d)),
+                                      Hq, Hkv, D, dict(attn=1 + w(d), ffn=1 + w(d), attn_post=1 + w(d), ffn_post=1 + w(d), **head_norms()),
                                       angle.cos(), angle.sin(), group=64) for _ in range(n_blocks)]
         self.embed, self.last_norm = w(vocab, d, scale=1.0), 1 + w(d)
         self.head = P.QuantLinear(w(vocab, d), group=64)
-        self.caches = [P.PagedCache.create(1, max_len, Hkv, D, page_size=32, device=dev) for _ in range(n_blocks)]
+        self.caches = [cache.create(1, max_len, Hkv, D, page_size=page, device=dev) for _ in range(n_blocks)]
         self.len = 0      # the caches' length, which the program knows without asking the device
 
     def logits(self, tokens, positions=None, mask=None):
@@ -77,11 +79,30 @@ class Model:
         return tokens, parents
 
 
-def decode(model, prompt, n_new):
-    """n_new greedy tokens; (tokens, steps of the model it took)."""
+def decode(model, prompt, n_new, temperature=0.0, seed=0):
+    """n_new tokens, greedy unless a temperature is given; (tokens, steps of the model it took)."""
+    g = torch.Generator(device="cuda:0").manual_seed(seed)
+    verifier = P.DraftVerifier("cuda:0")
+
+    def verify(logits, off, tokens, parents=None):
+        """(accepted tokens' places, the token after them)."""
+        n = len(tokens)
+        u = u_next = heat = None
+        if temperature > 0:
+            u, u_next = torch.rand(n, device="cuda:0", generator=g), torch.rand(1, device="cuda:0", generator=g)
+            heat = torch.full((1,), temperature, device="cuda:0")
+
+        def ints(x):
+            return None if x is None else torch.tensor(x, dtype=torch.int32, device="cuda:0")
+        keep, count, after = verifier(logits, ints(tokens), off, n, parents=ints(parents), u=u, u_next=u_next, temperature=heat)
+        path = keep[0, :int(count)].tolist()
+        if verifier.status_value():
+            raise P.MoEError("verification reported status %d" % verifier.status_value())
+        return path, int(after)
     logits, off = model.logits(torch.tensor(prompt, device="cuda:0"))
     model.keep(off, list(range(len(prompt))))
-    out, steps = [int(logits[-1].argmax())], 1
+    one = torch.tensor([0, 1], dtype=torch.int32, device="cuda:0")
+    out, steps = [verify(logits[-1:], one, prompt[-1:])[1]], 1
     while len(out) < n_new:
         tokens, parents = model.draft(out[-1])
         depth = []
@@ -89,13 +110,8 @@ def decode(model, prompt, n_new):
             depth.append(0 if p < 0 else depth[p] + 1)
         positions = torch.tensor([model.len + x for x in depth], dtype=torch.int32, device="cuda:0")
         logits, off = model.logits(torch.tensor(tokens, device="cuda:0"), positions, P.tree_mask([parents]))
-        choice, path = logits.argmax(1).tolist(), [0]
-        while True:      # down the tree as long as a draft is what the model chose
-            out.append(choice[path[-1]])
-            child = [i for i, p in enumerate(parents) if p == path[-1] and tokens[i] == out[-1]]
-            if not child:
-                break
-            path.append(child[0])
+        path, after = verify(logits, off, tokens, parents)
+        out += [tokens[i] for i in path[1:]] + [after]
         model.keep(off, path)
         steps += 1
     return out[:n_new], steps
@@ -121,6 +137,10 @@ def main():
     same = sum(a == b for a, b in zip(out, want))
     assert all(x.status_value() == 0 for m in (model, plain) for x in m.caches + m.blocks)
     print("%d tokens in %d steps of the model; %d of them as one token at a time gives" % (len(out), steps, same))
+    small = Model(cache=P.QuantPagedCache, page=64)
+    drawn, steps8 = decode(small, prompt, 60, temperature=0.8)
+    assert all(x.status_value() == 0 for x in small.caches + small.blocks)
+    print("drawn at temperature 0.8 over caches in 8 bits: %d tokens in %d steps" % (len(drawn), steps8))
     return out, want, steps
 
 

@@ -6,13 +6,15 @@
 // grows by S, from c = 0, S = 1.  One refusal costs one sum over a row, and its sums by chunk of
 // the vocabulary are what the next token is drawn from if the walk ends there.  Without
 // probabilities a refusal takes one token out, and nothing is summed before the end.
-//   stats_kernel   per row and chunk: maximum and sum of exponentials, or the first of the
+//   stats_kernel   per row and block of it: maximum and sum of exponentials, or the first of the
 //                  largest                                      (reads every logit once)
 //   walk_kernel    per sequence: rows' statistics, drafts' probabilities, the walk to its end or
 //                  to the first sum that it needs
-//   pass_kernel    per sequence and chunk: that sum; the last workgroup of a sequence adds up and
-//                  walks on, and at the end of the walk draws.  Launched once for chains and picked
-//                  drafts, a few times for drawn trees; the last launch sees to the rest alone.
+//   pass_kernel    per sequence and chunk of the vocabulary: that sum; the last workgroup of a
+//                  sequence adds up and walks on, and at the end of the walk draws.  Launched once
+//                  for chains and picked drafts, a few times for drawn trees; the last launch sees
+//                  to the rest alone.  Where there are few blocks, each workgroup of the first pass
+//                  begins the walk itself, and no walk_kernel is launched.
 #include <algorithm>
 
 #include "elem.hpp"
@@ -117,6 +119,7 @@ __global__ void __launch_bounds__(kThreads) stats_kernel(Args a) {
   bool ok;
   const Seq s = sequence(a, b, ok);
   const float heat = heat_of(a, b);
+  if (block == 0 && i == 0 && tid == 0) a.arrived[static_cast<int64_t>(b) * kApart] = 0;
   if (i >= s.n) return;
   const bool greedy = !a.u || heat == 0.f;
   const int64_t row = s.off + i;
@@ -183,20 +186,25 @@ __global__ void __launch_bounds__(kThreads) stats_kernel(Args a) {
 // a row's probability of a logit, in 64 bits
 __device__ __forceinline__ double prob(double x, float top, double sum, double heat) { return exp((x - top) / heat) / sum; }
 
-// Drafts of a sequence as the walk reads them, in LDS that is sized for the call's longest.
-constexpr int kDraftBytes = 32;
+// A sequence's drafts as the walk reads them, in LDS that is sized for the call's longest.
+constexpr int kDraftBytes = 48;
+constexpr int kOpen = INT32_MIN;   // of `next`: not decided
 struct Drafts {
   double *prob, *sum;     // at the parent; the sum of its own row, NaN: no distribution
-  float *share, *u;       // of the draft distribution at the parent
-  int *above, *token;
+  float *share, *u, *top; // of the draft distribution at the parent; its own row's maximum
+  int *above, *token, *arg, *path, *taken;   // parents; first of the largest; kept rows; refused tokens
 
   __device__ __forceinline__ Drafts(char* lds, int most) {
     prob = reinterpret_cast<double*>(lds);
     sum = prob + most;
     share = reinterpret_cast<float*>(sum + most);
     u = share + most;
-    above = reinterpret_cast<int*>(u + most);
+    top = u + most;
+    above = reinterpret_cast<int*>(top + most);
     token = above + most;
+    arg = token + most;
+    path = arg + most;
+    taken = path + most;
   }
 };
 
@@ -209,8 +217,8 @@ __device__ __forceinline__ int child(const Drafts& d, int n, int cur, int from, 
   return -1;
 }
 
-// Walks on, in one wave: to the end, or to a refusal that needs a sum.
-__device__ __forceinline__ void walk(const Args& a, int b, const Seq& s, const Drafts& d, State& st, int lane) {
+// Walks on, in one wave: to the end, or to a refusal that needs a sum.  Rows that are kept go to `path`.
+__device__ __forceinline__ void walk(const Args& a, const Seq& s, const Drafts& d, State& st, int* path, int* next, int lane) {
   for (;;) {
     const int i = child(d, s.n, st.cur, st.at + 1, lane);
     if (i < 0) {
@@ -236,7 +244,7 @@ __device__ __forceinline__ void walk(const Args& a, int b, const Seq& s, const D
       if (!yes && !again) st.s -= p;
     }
     if (yes) {
-      if (lane == 0) a.keep[static_cast<int64_t>(b) * a.max_new + st.count] = i;
+      if (lane == 0) path[st.count] = i;
       st.cur = i;
       st.count++;
       st.c = 0.;
@@ -244,7 +252,7 @@ __device__ __forceinline__ void walk(const Args& a, int b, const Seq& s, const D
       if (d.sum[i] != d.sum[i]) {   // nothing to go on with
         if (lane == 0) {
           report(a, MOE_ERR_RANGE);
-          a.next[b] = -1;
+          *next = -1;
         }
         st.need = kDone;
         return;
@@ -257,15 +265,10 @@ __device__ __forceinline__ void walk(const Args& a, int b, const Seq& s, const D
   }
 }
 
-__global__ void __launch_bounds__(1024) walk_kernel(Args a, int most) {
-  extern __shared__ __attribute__((aligned(16))) char lds[];
-  const Drafts d(lds, most);
-  float* tops = reinterpret_cast<float*>(lds + most * kDraftBytes);
-  int* args = reinterpret_cast<int*>(tops + most);
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, threads = blockDim.x;
-  bool ok;
-  const Seq s = sequence(a, b, ok);
-  if (!ok && tid == 0) report(a, MOE_ERR_SLOT);
+// The walk's beginning, by a whole workgroup: statistics of the sequence's rows, its drafts'
+// probabilities, and on to the first sum.  st, next and the drafts are in LDS.
+__device__ __forceinline__ void begin(const Args& a, int b, const Seq& s, const Drafts& d, State* out, int* next, int tid, int threads) {
+  const int lane = tid % kWave;
   const float heat = heat_of(a, b);
   const bool greedy = !a.u || heat == 0.f, cold = !greedy && (!(heat > 0.f) || heat == INFINITY);
   const float rate = greedy ? 0.f : rate_of(heat);
@@ -282,7 +285,6 @@ __global__ void __launch_bounds__(1024) walk_kernel(Args a, int most) {
     d.prob[i] = p < 0 || greedy ? 0. : load_elem(a.logits, (s.off + p) * a.ld + x, a.type);   // the logit, for now
     d.share[i] = p < 0 || greedy || !a.draft ? 0.f : load_elem(a.draft, (s.off + p) * a.ld_draft + x, a.draft_type);
   }
-  for (int i = tid; i < a.max_new; i += threads) a.keep[static_cast<int64_t>(b) * a.max_new + i] = i || s.n == 0 ? -1 : 0;
   // rows' blocks: `wide` lanes to a row, a power of two
   const int wide = a.blocks >= kWave ? kWave : 1 << (32 - __builtin_clz(a.blocks) - ((a.blocks & (a.blocks - 1)) == 0));
   for (int i0 = tid / kWave * (kWave / wide); i0 < s.n; i0 += threads / wide) {
@@ -312,58 +314,85 @@ __global__ void __launch_bounds__(1024) walk_kernel(Args a, int most) {
     if (cold || !(__builtin_fabsf(top) < INFINITY)) sum = __builtin_nan("");
     if (live && c0 == 0) {
       d.sum[i] = sum;
-      tops[i] = top;
-      args[i] = arg;
-      a.row_sum[s.off + i] = sum;
-      a.row_top[s.off + i] = top;
+      d.top[i] = top;
+      d.arg[i] = arg;
     }
   }
   __syncthreads();
   if (!greedy) {
     for (int i = tid; i < s.n; i += threads) {
       const int p = d.above[i];
-      if (p >= 0) d.prob[i] = prob(d.prob[i], tops[p], d.sum[p], heat);
-      a.prob[s.off + i] = d.prob[i];
-      a.share[s.off + i] = d.share[i];
-      a.above[s.off + i] = p;
+      if (p >= 0) d.prob[i] = prob(d.prob[i], d.top[p], d.sum[p], heat);
     }
     __syncthreads();
   }
-  if (tid >= kWave) return;
-  State st{0., 1., 0., 0.f, 0, 0, s.n > 0, kDone, 0};
-  if (s.n == 0 || d.sum[0] != d.sum[0]) {
+  if (tid < kWave) {
+    State st{0., 1., 0., 0.f, 0, 0, s.n > 0, kDone, 0};
     if (lane == 0) {
-      if (s.n) report(a, MOE_ERR_RANGE);
-      a.next[b] = -1;
+      *next = kOpen;
+      if (s.n) d.path[0] = 0;
     }
-  } else if (greedy) {
-    for (int j0 = 1; j0 < s.n;) {   // drafts below cur whose token is the largest
-      const int j = j0 + lane;
-      const uint64_t kids = __ballot(j < s.n && d.above[j] == st.cur && d.token[j] == args[st.cur]);
-      if (!kids) {
-        j0 += kWave;
-        continue;
+    if (s.n == 0 || d.sum[0] != d.sum[0]) {
+      if (lane == 0) {
+        if (s.n) report(a, MOE_ERR_RANGE);
+        *next = -1;
       }
-      st.cur = j0 + __builtin_ctzll(kids);
-      if (lane == 0) a.keep[static_cast<int64_t>(b) * a.max_new + st.count] = st.cur;
-      st.count++;
-      j0 = st.cur + 1;
-      if (d.sum[st.cur] != d.sum[st.cur]) break;
+    } else if (greedy) {
+      for (int j0 = 1; j0 < s.n;) {   // drafts below cur whose token is the largest
+        const int j = j0 + lane;
+        const uint64_t kids = __ballot(j < s.n && d.above[j] == st.cur && d.token[j] == d.arg[st.cur]);
+        if (!kids) {
+          j0 += kWave;
+          continue;
+        }
+        st.cur = j0 + __builtin_ctzll(kids);
+        if (lane == 0) d.path[st.count] = st.cur;
+        st.count++;
+        j0 = st.cur + 1;
+        if (d.sum[st.cur] != d.sum[st.cur]) break;
+      }
+      if (lane == 0) {
+        const bool none = d.sum[st.cur] != d.sum[st.cur];
+        if (none) report(a, MOE_ERR_RANGE);
+        *next = none ? -1 : d.arg[st.cur];
+      }
+    } else {
+      walk(a, s, d, st, d.path, next, lane);
+      st.sum = d.sum[st.cur];
+      st.top = d.top[st.cur];
     }
-    if (lane == 0) {
-      const bool none = d.sum[st.cur] != d.sum[st.cur];
-      if (none) report(a, MOE_ERR_RANGE);
-      a.next[b] = none ? -1 : args[st.cur];
-    }
-  } else {
-    walk(a, b, s, d, st, lane);
-    st.sum = d.sum[st.cur];
-    st.top = tops[st.cur];
+    if (lane == 0) *out = st;
   }
-  if (lane == 0) {
+  __syncthreads();
+}
+
+// What a beginning leaves: the kept rows, and, where the walk goes on in another launch, the drafts.
+__device__ __forceinline__ void write_walk(const Args& a, int b, const Seq& s, const Drafts& d, const State& st, int next, bool on, int tid, int threads) {
+  for (int i = tid; i < a.max_new; i += threads) a.keep[static_cast<int64_t>(b) * a.max_new + i] = i < st.count ? d.path[i] : -1;
+  for (int i = tid; on && i < s.n; i += threads) {
+    a.prob[s.off + i] = d.prob[i];
+    a.share[s.off + i] = d.share[i];
+    a.above[s.off + i] = d.above[i];
+    a.row_sum[s.off + i] = d.sum[i];
+    a.row_top[s.off + i] = d.top[i];
+  }
+  if (tid == 0 && next != kOpen) a.next[b] = next;
+}
+
+__global__ void __launch_bounds__(1024) walk_kernel(Args a, int most) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  __shared__ State st;
+  __shared__ int next;
+  const Drafts d(lds, most);
+  const int b = blockIdx.x, tid = threadIdx.x;
+  bool ok;
+  const Seq s = sequence(a, b, ok);
+  if (!ok && tid == 0) report(a, MOE_ERR_SLOT);
+  begin(a, b, s, d, &st, &next, tid, blockDim.x);
+  write_walk(a, b, s, d, st, next, st.need != kDone, tid, blockDim.x);
+  if (tid == 0) {
     a.n_keep[b] = st.count;
     a.state[b] = st;
-    a.arrived[static_cast<int64_t>(b) * kApart] = 0;
   }
 }
 
@@ -441,20 +470,39 @@ __device__ __forceinline__ int first_past(double mine, double up, double aim, in
 __device__ __forceinline__ void put_total(double* p, double v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ double read_total(const double* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-template <int EACH>
+// FIRST: begins the walk.
+template <int EACH, bool FIRST>
 __global__ void __launch_bounds__(kThreads) pass_kernel(Args a, int most, int last) {
-  extern __shared__ __attribute__((aligned(16))) char lds[];   // drafts, or the tokens that are taken out
-  __shared__ int n_taken;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  __shared__ int n_taken, next;
   const Drafts d(lds, most);
-  const Taken taken{&n_taken, reinterpret_cast<int*>(lds + most * kDraftBytes)};
+  const Taken taken{&n_taken, d.taken};
   __shared__ double parts[kWaves], carry;
   __shared__ int marks[2 * kWaves], chosen;
   __shared__ State shared;
   const int chunk = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid % kWave;
-  State st = a.state[b];
-  if (st.need == kDone) return;
+  State st;
+  Seq s;
   bool ok;
-  const Seq s = sequence(a, b, ok);
+  if constexpr (FIRST) {      // every workgroup of the sequence the same
+    s = sequence(a, b, ok);
+    if (!ok && tid == 0) report(a, MOE_ERR_SLOT);
+    begin(a, b, s, d, &shared, &next, tid, kThreads);
+    st = shared;
+    if (st.need == kDone) {
+      if (chunk == 0) write_walk(a, b, s, d, st, next, false, tid, kThreads);
+      if (chunk == 0 && tid == 0) {
+        a.n_keep[b] = st.count;
+        a.state[b] = st;
+      }
+      return;
+    }
+  } else {
+    st = a.state[b];
+    if (st.need == kDone) return;
+    s = sequence(a, b, ok);
+    if (tid == 0) next = kOpen;
+  }
   Row r;
   r.heat = heat_of(a, b);
   // what to sum next: sets r, and the tokens that are taken out of cur's row
@@ -469,7 +517,7 @@ __global__ void __launch_bounds__(kThreads) pass_kernel(Args a, int most, int la
     __syncthreads();
     if (st.s > 0.)
       for (int j = st.cur + 1 + tid; j < s.n; j += kThreads)
-        if (a.above[s.off + j] == st.cur) taken.token[atomicAdd(&n_taken, 1)] = a.tokens[s.off + j];
+        if ((FIRST ? d.above[j] : a.above[s.off + j]) == st.cur) taken.token[atomicAdd(&n_taken, 1)] = a.tokens[s.off + j];
     __syncthreads();
   };
   auto chunk_sum = [&](int c) {
@@ -499,7 +547,8 @@ __global__ void __launch_bounds__(kThreads) pass_kernel(Args a, int most, int la
   // the last workgroup of the sequence: add up, and walk on
   if (tid == 0) a.arrived[static_cast<int64_t>(b) * kApart] = 0;
   const int each = (a.chunks + kThreads - 1) / kThreads;   // chunks of a thread, side by side
-  bool loaded = false;
+  bool loaded = FIRST;
+  int* path = FIRST ? d.path : a.keep + static_cast<int64_t>(b) * a.max_new;
   for (bool summed = true;;) {
     if (!summed) {   // alone, a chunk to a wave
       aim_at();
@@ -536,6 +585,7 @@ __global__ void __launch_bounds__(kThreads) pass_kernel(Args a, int most, int la
           d.above[i] = a.above[s.off + i];
           d.token[i] = a.tokens[s.off + i];
           d.sum[i] = a.row_sum[s.off + i];
+          d.top[i] = a.row_top[s.off + i];
         }
         loaded = true;
       }
@@ -545,11 +595,11 @@ __global__ void __launch_bounds__(kThreads) pass_kernel(Args a, int most, int la
       }
       __syncthreads();
       if (tid < kWave) {
-        walk(a, b, s, d, st, lane);
+        walk(a, s, d, st, path, &next, lane);
         if (lane == 0) {
           shared = st;
           shared.sum = d.sum[st.cur];
-          shared.top = a.row_top[s.off + st.cur];
+          shared.top = d.top[st.cur];
         }
       }
       __syncthreads();
@@ -604,6 +654,9 @@ __global__ void __launch_bounds__(kThreads) pass_kernel(Args a, int most, int la
     if (st.need == kDone || !last) break;
     summed = false;
   }
+  __syncthreads();
+  if (FIRST) write_walk(a, b, s, d, st, next, st.need != kDone, tid, kThreads);
+  else if (tid == 0 && next != kOpen) a.next[b] = next;
   if (tid == 0) {
     a.n_keep[b] = st.count;
     a.state[b] = st;
@@ -656,6 +709,12 @@ void launch_stats(bool wide, int most, hipStream_t s, const Args& a) {
   const dim3 grid(a.blocks, most, a.n_seqs), block(kThreads);
   if (wide) hipLaunchKernelGGL((stats_kernel<TYPE, 32>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((stats_kernel<TYPE, 16>), grid, block, 0, s, a);
+}
+
+template <int EACH>
+void launch_pass(bool first, dim3 grid, int bytes, hipStream_t s, const Args& a, int most, int last) {
+  if (first) hipLaunchKernelGGL((pass_kernel<EACH, true>), grid, dim3(kThreads), bytes, s, a, most, last);
+  else hipLaunchKernelGGL((pass_kernel<EACH, false>), grid, dim3(kThreads), bytes, s, a, most, last);
 }
 
 int check_sizes(int32_t n_seqs, int32_t n_tokens, int32_t max_new, int32_t vocab) {
@@ -745,29 +804,31 @@ extern "C" int moe_draft_verify(const void* logits, int32_t logits_type, int64_t
   a.draft_type = draft_type;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int most = std::min(max_new, n_tokens);
-  const dim3 block(kThreads);
   if (most > 0) {
     const bool wide = each_of(n_tokens, vocab) == 32;
     if (logits_type == MOE_TYPE_FP32) launch_stats<MOE_TYPE_FP32>(wide, most, s, a);
     else if (logits_type == MOE_TYPE_BF16) launch_stats<MOE_TYPE_BF16>(wide, most, s, a);
     else launch_stats<MOE_TYPE_FP16>(wide, most, s, a);
   }
-  // a lane for every block of a sequence's rows, if that takes no more than a workgroup
-  const int threads = static_cast<int64_t>(most) * a.blocks > kThreads ? 1024 : kThreads;
-  hipLaunchKernelGGL(walk_kernel, dim3(n_seqs), dim3(threads), most * (kDraftBytes + 8), s, a, most);
+  // The first pass begins the walk where that takes each of its workgroups no more than a few loads (one
+  // chain of 4 over 32000 tokens 17.4 us, with a launch for it 19.5; 64 chains of 7 29.4 and 31.4); else a launch with a lane for every
+  // block of a sequence's rows, if that takes no more than a workgroup.
+  const int64_t parts = static_cast<int64_t>(most) * a.blocks;
+  const bool with_pass = most > 0 && u && parts <= 512;
+  if (!with_pass) hipLaunchKernelGGL(walk_kernel, dim3(n_seqs), dim3(parts > kThreads ? 1024 : kThreads), most * kDraftBytes, s, a, most);
   if (most > 0 && u) {
     // A drawn tree takes a pass for each refusal of its walk.  What the launches leave is summed by one
     // workgroup (0.7 us a chunk); one with nothing to do takes 2 us.  16 trees of 31 over 131072 tokens:
     // 80 us with 4, 85 with 6, or, where a walk refuses 5 times, 127 with 4, 93 with 6.
     const int passes = draft && parents ? std::min(most, a.chunks == 1 ? 1 : a.chunks <= 4 ? 3 : a.chunks <= 32 ? 4 : 6) : 1;
-    const int bytes = most * (kDraftBytes + 4);
+    const int bytes = most * kDraftBytes;
     const int each = pass_each_of(n_seqs, vocab);
     const dim3 grid(a.chunks, n_seqs);
     for (int i = 0; i < passes; i++) {
-      const int last = i == passes - 1;
-      if (each == 4) hipLaunchKernelGGL(pass_kernel<4>, grid, block, bytes, s, a, most, last);
-      else if (each == 8) hipLaunchKernelGGL(pass_kernel<8>, grid, block, bytes, s, a, most, last);
-      else hipLaunchKernelGGL(pass_kernel<16>, grid, block, bytes, s, a, most, last);
+      const bool first = with_pass && i == 0;
+      if (each == 4) launch_pass<4>(first, grid, bytes, s, a, most, i == passes - 1);
+      else if (each == 8) launch_pass<8>(first, grid, bytes, s, a, most, i == passes - 1);
+      else launch_pass<16>(first, grid, bytes, s, a, most, i == passes - 1);
     }
   }
   return launch_status(s);
