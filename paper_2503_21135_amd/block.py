@@ -301,6 +301,8 @@ class DraftVerifier:
 
         Returns int32 (keep [sequences][max_new], n_keep, next_token [sequences]); keep and n_keep
         are what PagedCache.keep takes: the known token's row and the accepted drafts'."""
+        if not logits.is_cuda or logits.dim() != 2:
+            raise MoEError("logits must be a device tensor [rows][vocabulary]")
         B, key = new_off.shape[0] - 1, (new_off.shape[0], logits.shape[0], max_new, logits.shape[1])
         need = self._need.get(key)
         if need is None:

@@ -466,8 +466,13 @@ __device__ __forceinline__ int first_past(double mine, double up, double aim, in
   return at;
 }
 
-// sums that one workgroup of a launch writes and another reads
-__device__ __forceinline__ void put_total(double* p, double v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// Sums that one workgroup of a launch writes and another reads.  An exchange has been performed where
+// the whole device sees it once its old value is back, which the wait is for.
+__device__ __forceinline__ void put_total(double* p, double v) {
+  auto* at = reinterpret_cast<unsigned long long*>(p);
+  const unsigned long long old = __hip_atomic_exchange(at, __builtin_bit_cast(unsigned long long, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  asm volatile("s_waitcnt vmcnt(0)" : : "v"(old) : "memory");
+}
 __device__ __forceinline__ double read_total(const double* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 // FIRST: begins the walk.
@@ -536,10 +541,9 @@ __global__ void __launch_bounds__(kThreads) pass_kernel(Args a, int most, int la
   const double mine = chunk_sum(chunk);
   if (tid == 0) {
     put_total(&total[chunk], mine);
-    // All that workgroups of one launch hand over is that sum, stored past the XCD's L2: once it has
-    // arrived, the count may go up.  (A release at device scope writes the whole L2 back, for each
-    // workgroup: 64 sequences by 32 chunks 46 us that way.)
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // That sum is all that workgroups of one launch hand over, so the count may go up once it is there.
+    // (A release at device scope writes the whole L2 back, for each workgroup: 64 sequences by 32
+    // chunks 46 us that way, 24 this way.)
     chosen = __hip_atomic_fetch_add(&a.arrived[static_cast<int64_t>(b) * kApart], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
   }
   __syncthreads();

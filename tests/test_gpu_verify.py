@@ -233,6 +233,49 @@ def test_draft_and_model_agree():
     check(wide, 7)
 
 
+@pytest.mark.parametrize("heat", [1e-45, 1e-38, 1e-20, 1e-3, 1e3, 3e38])
+def test_temperatures_of_any_size(heat):
+    s = drafts([5] * 10, 3000, "wide", 19, FP32, FP32)
+    s["logits"][3] *= 1e30
+    check(s, 5, heat=torch.full((10,), heat, device="cuda"))
+
+
+def test_graphs_and_eager_calls_work_in_memory_of_their_own(monkeypatch):
+    from paper_2503_21135_amd import api
+    s = drafts([8] * 6, 5000, "wide", 16, FP32, FP32)
+    v, off, par, seen = P().DraftVerifier(), i32(s["off"]), i32(s["parents"]), []
+    call = api.moe_draft_verify
+
+    def noted(*args):
+        ws = next(t for t in args if torch.is_tensor(t) and t.dtype is torch.uint8)
+        seen.append((ws.data_ptr(), ws.data_ptr() + ws.numel()))
+        return call(*args)
+    monkeypatch.setattr(api, "moe_draft_verify", noted)
+
+    def step():
+        return v(s["logits"], s["tokens"], off, 8, parents=par, draft_probs=s["draft"], u=s["u"], u_next=s["last"])
+    want, graphs = step(), []
+    torch.cuda.synchronize()
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = step()
+        graphs.append((g, out))
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        other = step()
+    assert len(seen) == 4 and all(b <= c or d <= a for i, (a, b) in enumerate(seen) for c, d in seen[:i])
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for _ in range(10):
+        for (g, _), st in zip(graphs, streams):
+            with torch.cuda.stream(st):
+                g.replay()
+        more = step()
+        torch.cuda.synchronize()
+        for out in [more, other] + [o for _, o in graphs]:
+            assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
 def test_greedy_ties_go_to_the_first():
     logits = torch.zeros(6, 9000, device="cuda")
     logits[:, [8999, 5000, 4096, 17]] = 4.0
