@@ -777,9 +777,11 @@ int moe_qcache_read(const moe_qcache_t* C, const int32_t* table, int32_t max_pag
  * moe_qcache_attention, moe_qcache_attention_plan -- moe_tree_attention over a cache in
  * 8 bits, with the same arguments and meaning.  The codes enter both products as they are,
  * exact in the 16-bit operand types; a key's scale multiplies its fp32 scores, a value's
- * scale its softmax weight, which then is rounded to fp16 (and counts as rounded in the
- * weights' sum; below 2^-32 of the largest product of weight and scale that the row sees
- * it may count as zero).  Results are bitwise reproducible.
+ * scale its softmax weight, which then enters the second product rounded to fp16, or, for
+ * fp16 outputs up to 32 rows per key/value head (max_new * n_q_heads / n_heads; 16 at
+ * head_dim 256), as a rounded weight and the rounded rest.  (Below 2^-32 of the row's largest
+ * such product of weight and scale it may count as zero there.)  The weights' sum is of
+ * fp32 weights, none of them left out.  Results are bitwise reproducible.
  */
 int moe_qcache_attention_plan(const moe_qcache_t* C, int32_t n_q_heads, int32_t n_seqs,
                               int32_t max_new, int32_t max_len, int32_t* n_split, size_t* ws_bytes);

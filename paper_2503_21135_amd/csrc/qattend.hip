@@ -176,6 +176,13 @@ __device__ __forceinline__ f32x4 from_lanes(float v, int kt) {
 // Many rows (RW > 1): RW waves on 16 RT rows each by KW groups of keys; a group's waves read its
 // tiles once, side by side, and widen the codes once on their way into LDS (double-buffered,
 // one barrier a tile).
+// Few rows are bound by HBM: 64 single tokens by 32 query and 8 key heads of 128 over up to 4096, 415 MB,
+// 83 us, 5.0 TB/s and up to 6.1 for longer contexts.  The next tile's
+// keys load behind this one's products (else 94 us); a third wave a SIMD would spill (105).
+// Many rows are bound by phases that hardly overlap: 4 trees of 64 over up to 32768 147 us (0.56 PFLOP/s;
+// matrix instructions a third of a busy CU's cycles, vector ones half, LDS a third).  Tried for
+// them: one row tile's products among the other's softmax 178 us, two workgroups a CU 179, the two waves of
+// a SIMD half a tile apart 177, scales by lanes instead of LDS 170, s_setprio 172 (all against 161 then).
 template <int TYPE, int D, int RT, int RW, int KW>
 __global__ void __launch_bounds__(64 * RW * KW, RW * KW == 8 || (RW == 1 && D <= 128) ? 2 : 1) attend_kernel(QArgs a) {
   typedef elem_t<TYPE> E;
