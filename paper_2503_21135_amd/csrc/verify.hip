@@ -211,6 +211,8 @@ struct Drafts {
   }
 };
 
+__device__ __forceinline__ float clamped(float u) { return fminf(fmaxf(u, 0.f), 0x1.fffffep-1f); }
+
 // the first draft below row `cur` from `from` on, or -1; in one wave
 __device__ __forceinline__ int child(const Drafts& d, int n, int cur, int from, int lane) {
   for (int j0 = from; j0 < n; j0 += kWave) {
@@ -221,21 +223,45 @@ __device__ __forceinline__ int child(const Drafts& d, int n, int cur, int from, 
 }
 
 // Walks on, in one wave: to the end, or to a refusal that needs a sum.  Rows that are kept go to `path`.
+// A lane holds one of 64 drafts, whose index only grows, and whether it is accepted as the first that is
+// tested below its parent is known for all of them at once, so that a step of a chain is a ballot and
+// a few scalar instructions (the longest walks of 64 chains of 7 4.8 us with a draft read from LDS at a time, 3.2 this way).
 __device__ __forceinline__ void walk(const Args& a, const Seq& s, const Drafts& d, State& st, int* path, int* next, int lane) {
+  int above = -2, base = -1, from = st.at + 1;
+  uint64_t first = 0, lost = 0;   // of the 64: accepted if no elder was refused; without a distribution
+  bool elder = false;             // of cur's drafts, one was refused here
   for (;;) {
-    const int i = child(d, s.n, st.cur, st.at + 1, lane);
-    if (i < 0) {
+    if (from >= s.n) {
       st.need = kDraw;
       return;
     }
+    if ((from & -kWave) != base) {
+      base = from & -kWave;
+      const int j = base + lane;
+      bool yes = false, bad = false;
+      above = -2;
+      if (j < s.n) {
+        above = d.above[j];
+        const double p = d.prob[j], u = clamped(d.u[j]), w = a.draft ? d.share[j] : 1.;
+        yes = u * w < p;
+        bad = d.sum[j] != d.sum[j];
+      }
+      first = __ballot(yes);
+      lost = __ballot(bad);
+    }
+    const uint64_t kids = __ballot(above == st.cur) & ~0ull << (from - base);
+    if (!kids) {
+      from = base + kWave;
+      continue;
+    }
+    const int bit = __builtin_ctzll(kids), i = base + bit;
     st.at = i;
-    const double p = d.prob[i];
-    const float u = fminf(fmaxf(d.u[i], 0.f), 0x1.fffffep-1f);
-    bool yes;
-    if (a.draft) {
+    from = i + 1;
+    bool yes = first >> bit & 1;
+    if (a.draft && (st.c != 0. || st.s != 1.)) {
       const double w = d.share[i];
-      yes = u * w * st.s < p - st.c * w;
-    } else {
+      yes = clamped(d.u[i]) * w * st.s < d.prob[i] - st.c * w;
+    } else if (!a.draft && elder) {
       // taken out before, by an elder sibling
       bool again = false;
       for (int j0 = st.cur + 1; j0 < i; j0 += kWave) {
@@ -243,8 +269,8 @@ __device__ __forceinline__ void walk(const Args& a, const Seq& s, const Drafts& 
         again = again || (j < i && d.above[j] == st.cur && d.token[j] == d.token[i]);
       }
       again = __any(again);
-      yes = !again && u * st.s < p;
-      if (!yes && !again) st.s -= p;
+      if (again) continue;
+      yes = clamped(d.u[i]) * st.s < d.prob[i];
     }
     if (yes) {
       if (lane == 0) path[st.count] = i;
@@ -252,7 +278,8 @@ __device__ __forceinline__ void walk(const Args& a, const Seq& s, const Drafts& 
       st.count++;
       st.c = 0.;
       st.s = 1.;
-      if (d.sum[i] != d.sum[i]) {   // nothing to go on with
+      elder = false;
+      if (lost >> bit & 1) {   // nothing to go on with
         if (lane == 0) {
           report(a, MOE_ERR_RANGE);
           *next = -1;
@@ -262,8 +289,11 @@ __device__ __forceinline__ void walk(const Args& a, const Seq& s, const Drafts& 
       }
     } else if (a.draft) {
       st.need = kRefusal;
-      st.more = child(d, s.n, st.cur, i + 1, lane) >= 0;
+      st.more = (kids & kids - 1) != 0 || child(d, s.n, st.cur, base + kWave, lane) >= 0;
       return;
+    } else {
+      st.s -= d.prob[i];
+      elder = true;
     }
   }
 }
@@ -341,21 +371,22 @@ __device__ __forceinline__ void begin(const Args& a, int b, const Seq& s, const 
         *next = -1;
       }
     } else if (greedy) {
-      for (int j0 = 1; j0 < s.n;) {   // drafts below cur whose token is the largest
-        const int j = j0 + lane;
-        const uint64_t kids = __ballot(j < s.n && d.above[j] == st.cur && d.token[j] == d.arg[st.cur]);
-        if (!kids) {
-          j0 += kWave;
-          continue;
+      // a lane's draft is its parent's largest or not; along the path as walk() goes
+      bool none = false;
+      for (int base = 0; base < s.n && !none; base += kWave) {
+        const int j = base + lane, above = j > 0 && j < s.n ? d.above[j] : -1;
+        const bool hit = above >= 0 && d.token[j] == d.arg[above];
+        const uint64_t lost = __ballot(j < s.n && d.sum[j] != d.sum[j]);
+        for (uint64_t kids; (kids = __ballot(hit && above == st.cur)) != 0;) {
+          const int bit = __builtin_ctzll(kids);
+          st.cur = base + bit;
+          if (lane == 0) d.path[st.count] = st.cur;
+          st.count++;
+          none = lost >> bit & 1;
+          if (none) break;
         }
-        st.cur = j0 + __builtin_ctzll(kids);
-        if (lane == 0) d.path[st.count] = st.cur;
-        st.count++;
-        j0 = st.cur + 1;
-        if (d.sum[st.cur] != d.sum[st.cur]) break;
       }
       if (lane == 0) {
-        const bool none = d.sum[st.cur] != d.sum[st.cur];
         if (none) report(a, MOE_ERR_RANGE);
         *next = none ? -1 : d.arg[st.cur];
       }
@@ -411,15 +442,28 @@ struct Taken {   // tokens that were refused, in LDS
   int* token;
 };
 
+// 2^y for y <= 0, by its Taylor series in ln2 (y - rint(y)) up to the 11th power: off by 7e-15 of
+// itself at most, and a rounding of 2^-53 or two.  The library's exp takes about twice the
+// instructions, and a pass one a token: 64 chains of 7 28.7 us with it, 27.8 with this; 16 trees of 31 82.7 and 80.9.
+__device__ __forceinline__ double power(double y) {
+  constexpr double kTerms[12] = {1.0, 0.6931471805599453, 0.24022650695910072, 0.05550410866482158, 0.009618129107628477, 0.0013333558146428443, 0.0001540353039338161, 1.5252733804059841e-05, 1.321548679014431e-06, 1.01780860092397e-07, 7.054911620801123e-09, 4.4455382718708116e-10};   // (ln 2)^k / k!
+  y = fmax(y, -1100.);   // 0, of -infinity too
+  const double n = __builtin_rint(y), f = y - n;
+  double sum = kTerms[11];
+#pragma unroll
+  for (int k = 10; k >= 0; k--) sum = __fma_rn(sum, f, kTerms[k]);
+  return __builtin_ldexp(sum, static_cast<int>(n));
+}
+
 // a thread's tokens' parts, from `at` on
 template <int EACH>
 __device__ __forceinline__ void parts_of(const Args& a, const Row& r, const Taken& out, int at, double (&v)[EACH]) {
   float x[EACH], w[EACH];
   load_some(a.type, a.logits, r.row * a.ld + at, a.vocab - at, -INFINITY, x);
   if (r.c > 0.) load_some(a.draft_type, a.draft, r.row * a.ld_draft + at, a.vocab - at, 0.f, w);
-  const double inv = 1. / r.heat;
+  const double rate = 1.4426950408889634 / r.heat;
 #pragma unroll
-  for (int e = 0; e < EACH; e++) v[e] = exp((static_cast<double>(x[e]) - r.top) * inv);
+  for (int e = 0; e < EACH; e++) v[e] = power((static_cast<double>(x[e]) - r.top) * rate);
   if (r.c > 0.) {
     const double scale = 1. / r.sum;
 #pragma unroll
@@ -479,9 +523,9 @@ __device__ __forceinline__ void put_total(double* p, double v) {
 __device__ __forceinline__ double read_total(const double* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 // FIRST: begins the walk.
-// A chain of latencies bounds it.  64 chains of 7 18.4 us, of which the beginning (lengths, drafts, their
-// logits and probabilities) takes 5.8, the chunk's sum 3.1, handing it over 1.1, adding up 1.2, the draw 2.9;
-// a pass of a tree's 16 sequences 8.6.
+// A chain of latencies bounds it.  64 chains of 7 17.2 us, of which the beginning (lengths, drafts, their
+// logits and probabilities, the walk) takes 5.6, the chunk's sum 2.7, handing it over 1.1, adding up 1.1, the draw 2.7;
+// a pass of 16 trees' sequences 8.4.
 template <int EACH, bool FIRST>
 __global__ void __launch_bounds__(kThreads) pass_kernel(Args a, int most, int last) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -622,7 +666,7 @@ __global__ void __launch_bounds__(kThreads) pass_kernel(Args a, int most, int la
       draw = false;
     }
     if (draw) {
-      const double goal = static_cast<double>(fminf(fmaxf(a.u_next[b], 0.f), 0x1.fffffep-1f)) * all;
+      const double goal = static_cast<double>(clamped(a.u_next[b])) * all;
       const int t = first_past(have, up, goal, marks, tid);
       if (tid == t) {    // the chunk among this thread's
         double before = up - have;
