@@ -113,11 +113,11 @@ __device__ __forceinline__ void load_floats(const float* p, float* f) {
 // together, so that norm and largest magnitude are sums and maxima over a few lanes.  The
 // tile's live tokens times its heads (the key's and the queries') are dealt out over the
 // workgroup: a tree of few tokens has its heads side by side (one head of all 64 slots at a time: 32
-// trees 15.9 us instead of 13.5, one token 4.7 instead of 3.4).  What the row's place alone tells is on
+// trees 15.9 us instead of 14, one token 4.7 instead of 3.4).  What the row's place alone tells is on
 // its way before positions and pages are known, and the next head's row during this one's arithmetic.
 // Prompts are bound by HBM: 8192 tokens of 32 query and 8 key heads of 128, 206 MB read and written,
-// take 49.1 us in 16 bits (4.2 TB/s).  Trees of drafts wait for a chain of dependent loads (lengths,
-// pages and positions, rows) and store their values a slot at a time: 32 trees of 16 to 32 tokens 13.5 us.
+// take 48.3 us in 16 bits (4.3 TB/s), 52.2 for 185 MB in 8, where a workgroup loads nothing while it quantizes.  Trees of drafts wait for a chain of dependent loads (lengths,
+// pages and positions, rows) and store their values a slot at a time: 32 trees of 16 to 32 tokens 14 us.
 // Values in workgroups of their own took the trees 15.8 us, four heads in registers at once the
 // prompt 50 instead of 40 in 8 bits (fewer waves), six waves a SIMD spill.
 template <int TYPE, int D, bool Q8>
@@ -130,6 +130,9 @@ __global__ void __launch_bounds__(4 * D) store_kernel(StoreArgs a) {
   __shared__ int64_t pages[kSlots / 32];            // first slot of each 32 in the head of its page, or -1
   __shared__ int where[kSlots];                     // position of each slot's token, or -1: no token, or one to skip
   __shared__ Two turned[D][kSlots / 2 + 2];
+  // w_k and w_q: in registers instead the prompt takes 51.9 us, not 50.7, and 8 of 300 to 600 tokens by 16 and 4
+  // heads of 256 52.3, not 49.6
+  __shared__ __attribute__((aligned(16))) float norms[2][D];
   const int s = blockIdx.y, g = blockIdx.z, tid = threadIdx.x;
   bool ok;
   const Seq q = sequence(a.b, s, ok);
@@ -167,6 +170,7 @@ __global__ void __launch_bounds__(4 * D) store_kernel(StoreArgs a) {
   };
   int item = tid / kItems;
   if (item < items) load_item(item);
+  if (const float* from = tid < D ? a.w_k : tid < 2 * D ? a.w_q : nullptr) norms[tid / D][tid % D] = from[tid % D];
 
   if (tid < kSlots) {
     const int slot = slot0 + tid;
@@ -183,26 +187,28 @@ __global__ void __launch_bounds__(4 * D) store_kernel(StoreArgs a) {
   }
   __syncthreads();
 
-  float cs[8], sn[8], w[16];     // of the last token, and of the last head's kind
-  int o_of = -1, kind_of = -1;
+  float cs[8], sn[8];
+  int o_of = -1;        // the token that they are of
   for (; item < items; item += kSlots) {
-    const int head = item / n_live, o = o_first + (item - head * n_live), pos = where[o], kind = head > 0;
+    const int head = item / n_live, o = o_first + (item - head * n_live), pos = where[o];
     float f[16];
     unpack<TYPE>(x, f);
     unpack<TYPE>(y, f + 8);
-    if (item + kSlots < items) load_item(item + kSlots);
-    if (pos < 0) continue;
-    if (turn && o != o_of) {
+    if (turn && pos >= 0 && o != o_of) {   // before the next row, which is not waited for then
       const int64_t at = static_cast<int64_t>(pos) * half + 8 * j;
       load_floats<8>(a.cos + at, cs);
       load_floats<8>(a.sin + at, sn);
       o_of = o;
     }
-    if (const float* from = head ? a.w_q : a.w_k) {
-      if (kind != kind_of) {
-        load_floats<8>(from + c0, w);
-        load_floats<8>(from + c1, w + 8);
-        kind_of = kind;
+    if (item + kSlots < items) load_item(item + kSlots);
+    if (pos < 0) continue;
+    if (head ? a.w_q : a.w_k) {
+      float w[16];
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(&norms[head > 0][(e < 8 ? c0 : c1) + e % 8]);
+#pragma unroll
+        for (int i = 0; i < 4; i++) w[e + i] = x[i];
       }
       float ss = 0.f;
 #pragma unroll
