@@ -138,6 +138,20 @@ def test_some_are_accepted_and_some_are_not():
     assert min(got) == 1 and max(got) >= 5 and refused_then_accepted > 20
 
 
+@pytest.mark.parametrize("kind,draft_dt", [("chain", FP32), ("chain", None), ("tree", FP32), ("tree", None)])
+def test_walks_longer_than_a_wave(kind, draft_dt):
+    new = [300, 1, 64, 65, 130]
+    s = drafts(new, 40, kind, 23, FP32, draft_dt, spread=4.0, noise=0.002, fan=70)
+    _, (_, n, _) = check(s, 300)
+    assert kind == "tree" or draft_dt is None or n[0] > 64
+    # every draft the likeliest below its parent: a chain is kept whole, of a tree the eldest
+    up = [s["off"][b] + (i - 1 if s["parents"] is None else s["parents"][s["off"][b] + i]) for b, m in enumerate(new) for i in range(m)]
+    s["tokens"] = s["logits"][torch.tensor(up, device="cuda").clamp(min=0)].argmax(1).int()
+    _, (_, n, _) = check(s, 300, greedy=True)
+    assert kind == "tree" or n == new
+    check(s, 300)     # picked ones are the same among siblings
+
+
 @pytest.mark.parametrize("kind,draft_dt", [("chain", FP32), ("wide", BF16), ("wide", None)])
 def test_ruled_out_tokens(kind, draft_dt):
     """-infinity, in all but a few places; and rows with an offset that suits no exponential."""
