@@ -78,9 +78,7 @@ class _Workspaces:
         self.device = device
         self._by_stream: Dict[int, torch.Tensor] = {}
 
-    def get(self, need: int, at: torch.Tensor, stream) -> Optional[torch.Tensor]:
-        if need == 0:
-            return None
+    def get(self, need: int, at: torch.Tensor, stream) -> torch.Tensor:
         if api._capturing(stream):
             return api._empty((need,), torch.uint8, self.device, stream)
         handle = api._stream(stream, at)
@@ -159,14 +157,7 @@ class PagedCache:
                                       positions, cos, sin, interleaved, self.status, stream)
 
     # the entry points of this kind of cache
-    def _plan(self, *sizes) -> int:
-        return api.moe_tree_attention_plan(self.desc, *sizes)[1]
-
-    def _attend(self, *args) -> None:
-        api.moe_tree_attention(*args)
-
-    def _keep(self, *args) -> None:
-        api.moe_cache_keep(*args)
+    _PLAN, _ATTEND, _KEEP = "moe_tree_attention_plan", "moe_tree_attention", "moe_cache_keep"
 
     def _workspace(self, n_q_heads: int, max_new: int, max_len: int, stream) -> Optional[torch.Tensor]:
         key = (n_q_heads, self.lens.shape[0], max_new, max_len)
@@ -174,8 +165,8 @@ class PagedCache:
         if need is None:
             if len(self._need) > 4096:
                 self._need.clear()
-            need = self._need[key] = self._plan(*key)
-        return self._ws.get(need, self.k, stream)
+            need = self._need[key] = getattr(api, self._PLAN)(self.desc, *key)[1]
+        return self._ws.get(need, self.k, stream) if need else None
 
     def attend(self, q: torch.Tensor, new_off: torch.Tensor, max_new: int, max_len: int,
                mask: Optional[torch.Tensor] = None, scale: Optional[float] = None,
@@ -185,9 +176,9 @@ class PagedCache:
         split).  scale: head_dim ** -0.5 unless given."""
         if out is None:
             out = api._empty(q.shape, q.dtype, q.device, stream)
-        self._attend(self.desc, self.table, self.lens, new_off, max_new, max_len, q, out,
-                     q.shape[2] ** -0.5 if scale is None else scale, mask,
-                     self._workspace(q.shape[1], max_new, max_len, stream), self.status, stream)
+        getattr(api, self._ATTEND)(self.desc, self.table, self.lens, new_off, max_new, max_len, q, out,
+                                   q.shape[2] ** -0.5 if scale is None else scale, mask,
+                                   self._workspace(q.shape[1], max_new, max_len, stream), self.status, stream)
         return out
 
     def keep(self, new_off: torch.Tensor, keep: torch.Tensor, n_keep: torch.Tensor,
@@ -197,7 +188,7 @@ class PagedCache:
         last layer's cache has been kept."""
         if len_out is None:
             len_out = api._empty(self.lens.shape, self.lens.dtype, self.lens.device, stream)
-        self._keep(self.desc, self.table, self.lens, new_off, keep, n_keep, len_out, self.status, stream)
+        getattr(api, self._KEEP)(self.desc, self.table, self.lens, new_off, keep, n_keep, len_out, self.status, stream)
         return len_out
 
 
@@ -250,14 +241,7 @@ class QuantPagedCache(PagedCache):
         api.moe_qcache_append(self.desc, self.table, self.lens, new_off, max_new, q, k, v, q_out, w_q, w_k, eps,
                               positions, cos, sin, interleaved, self.status, stream)
 
-    def _plan(self, *sizes) -> int:
-        return api.moe_qcache_attention_plan(self.desc, *sizes)[1]
-
-    def _attend(self, *args) -> None:
-        api.moe_qcache_attention(*args)
-
-    def _keep(self, *args) -> None:
-        api.moe_qcache_keep(*args)
+    _PLAN, _ATTEND, _KEEP = "moe_qcache_attention_plan", "moe_qcache_attention", "moe_qcache_keep"
 
     def read(self, first: torch.Tensor, row_off: torch.Tensor, max_rows: int, k_out: Optional[torch.Tensor] = None,
              v_out: Optional[torch.Tensor] = None, rows: Optional[int] = None, stream=None):

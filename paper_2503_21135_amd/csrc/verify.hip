@@ -799,8 +799,8 @@ extern "C" int moe_draft_verify(const void* logits, int32_t logits_type, int64_t
   if (int st = check_sizes(n_seqs, n_tokens, max_new, vocab)) return st;
   if (n_seqs == 0) return MOE_OK;
   if (!valid_type(logits_type) || (draft && !valid_type(draft_type)) || ld_logits < vocab || (draft && ld_draft < vocab)) return MOE_ERR_ARG;
-  if (!new_off || !n_keep || !next || (max_new > 0 && !keep) || !u != !u_next) return MOE_ERR_ARG;
-  if (n_tokens > 0 && (!logits || !tokens)) return MOE_ERR_ARG;
+  if (!new_off || !n_keep || !next || (max_new > 0 && !keep) || (u && !u_next)) return MOE_ERR_ARG;
+  if (n_tokens > 0 && (!logits || !tokens || !u != !u_next)) return MOE_ERR_ARG;
   if (!aligned_to(logits, type_bytes(logits_type)) || (draft && !aligned_to(draft, type_bytes(draft_type))) || !aligned_to(tokens, 4) ||
       !aligned_to(parents, 4) || !aligned_to(new_off, 4) || !aligned_to(temperature, 4) || !aligned_to(u, 4) || !aligned_to(u_next, 4) ||
       !aligned_to(keep, 4) || !aligned_to(n_keep, 4) || !aligned_to(next, 4) || !aligned_to(status, 4))

@@ -210,6 +210,19 @@ def test_tokens_parents_and_rows_out_of_range():
                 assert int(n2[b]) == 0 and int(x2[b]) == -1 and (k2[b] == -1).all()
 
 
+def test_no_rows_and_no_sequences():
+    v = P().DraftVerifier()
+    f = torch.zeros
+    keep, n, nxt = v(f(0, 50, device="cuda"), i32([]), i32([0]), 3)
+    assert keep.shape == (0, 3) and n.numel() == nxt.numel() == 0
+    for u in (None, f(0, device="cuda")):
+        keep, n, nxt = v(f(0, 50, device="cuda"), i32([]), i32([0, 0, 0]), 3, u=u, u_next=None if u is None else f(2, device="cuda"))
+        assert keep.tolist() == [[-1] * 3] * 2 and n.tolist() == [0, 0] and nxt.tolist() == [-1, -1]
+    keep, n, nxt = v(f(2, 50, device="cuda"), i32([1, 1]), i32([0, 1, 2]), 0)     # rows that max_new leaves out
+    assert keep.shape == (2, 0) and n.tolist() == [0, 0] and nxt.tolist() == [-1, -1]
+    assert v.status_value() == -5     # MOE_ERR_SLOT
+
+
 def test_edges_of_the_random_numbers():
     """0, the largest below 1, and numbers outside, which count as the nearest inside."""
     s = drafts([4] * 6, 50, "chain", 12, FP32, FP32)
