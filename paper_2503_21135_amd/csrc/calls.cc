@@ -144,7 +144,7 @@ int append_to(CALL call, PyObject* const* a, Py_ssize_t n) {
   const int dev = device_of(k, "k");
   if (!q != !q_out || !cos != (a[14] == Py_None)) refuse("q and q_out, cos and sin come in pairs");
   if (k.dim() != 3 || (q && q->dim() != 3)) refuse("q, k and v must be [tokens][heads][head_dim]");
-  if (cos && cos->dim() != 2) refuse("cos and sin must be [positions][half]");
+  if (cos && (cos->dim() != 2 || cos->numel() == 0)) refuse("cos and sin must be [positions][half], and not empty");
   const int64_t N = k.size(0), D = C->head_dim, Hq = q ? q->size(1) : 0, max_pos = cos ? cos->size(0) : 1, half = cos ? cos->size(1) : 0;
   const at::ScalarType t = type16(C->type);
   const Batch b = batch(a + 1, dev);
@@ -189,6 +189,7 @@ int attention(PyObject* const* a, Py_ssize_t n) {
   const int dev = device_of(q, "q");
   if (q.dim() != 3 || q.size(2) != C->head_dim) refuse(text("q must be [tokens][heads][%d], not %s", C->head_dim, described(q).c_str()));
   const int64_t N = q.size(0), Hq = q.size(1), words = mask ? (mask->dim() ? mask->size(-1) : 0) : 0, bytes = ws ? ws->numel() : 0;
+  if (mask && words < 1) refuse("mask must be [tokens][words], a word at least");   // an empty one has no address, as none
   const at::ScalarType t = type16(C->type);
   const Batch b = batch(a + 1, dev);
   const Heads qh = heads(&q, N, Hq, C->head_dim, t, dev, "q"), oh = heads(tensor(a[7], "out"), N, Hq, C->head_dim, t, dev, "out");

@@ -644,3 +644,18 @@ def test_tensors_that_do_not_fit_are_refused():
             cache.keep(**dict(dict(new_off=off, keep=keep if "keep" not in bad else None, n_keep=n), **bad))
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(was, (cache.k, cache.v, cache.k_scale, cache.v_scale)))
+
+
+def test_empty_masks_and_tables_are_refused():
+    """They have no address, which would say that there is none: a chain, no rotation."""
+    pkg = P()
+    cache, off = qbatch([10, 20], [2, 3], 64, 2, 64, BF16, 4)
+    kv, q = torch.randn(5, 2, 64, device="cuda").to(BF16), torch.randn(5, 4, 64, device="cuda").to(BF16)
+    with pytest.raises(pkg.MoEError, match="mask"):
+        cache.attend(q, off, 3, 23, mask=torch.zeros(5, 0, dtype=torch.int64, device="cuda"))
+    plain = pkg.PagedCache.create(2, 64, 2, 64)
+    for shape in ((0, 32), (50, 0)):
+        none = torch.zeros(*shape, device="cuda")
+        for c, kw in ((cache, {}), (plain, dict(w_k=torch.ones(64, device="cuda")))):
+            with pytest.raises(pkg.MoEError, match="cos"):
+                c.append(q, kv, kv, off, 3, cos=none, sin=none, **kw)
