@@ -269,7 +269,8 @@ class DraftVerifier:
 
     def status_value(self) -> int:
         """0, or MOE_ERR_SLOT once a token, parent or row was out of range, MOE_ERR_RANGE once a
-        row had no distribution (NaN, +infinity, nothing but -infinity); reads it back."""
+        row had no distribution (NaN, +infinity, nothing but -infinity, or a temperature that is
+        negative or not finite); reads it back."""
         return int(self.status.item())
 
     def __call__(self, logits: torch.Tensor, tokens: torch.Tensor, new_off: torch.Tensor, max_new: int,

@@ -303,7 +303,7 @@ __device__ __forceinline__ void walk(const Args& a, const Seq& s, const Drafts& 
 __device__ __forceinline__ void begin(const Args& a, int b, const Seq& s, const Drafts& d, State* out, int* next, int tid, int threads) {
   const int lane = tid % kWave;
   const float heat = heat_of(a, b);
-  const bool greedy = !a.u || heat == 0.f, cold = !greedy && (!(heat > 0.f) || heat == INFINITY);
+  const bool greedy = !a.u || heat == 0.f, cold = !(heat >= 0.f) || heat == INFINITY;   // cold: no temperature, greedy or not
   const float rate = greedy ? 0.f : rate_of(heat);
   for (int i = tid; i < s.n; i += threads) {
     int p = i ? (a.parents ? a.parents[s.off + i] : i - 1) : -1;
