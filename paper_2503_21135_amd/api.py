@@ -324,6 +324,8 @@ def moe_cache_append(desc: CacheDesc, table: torch.Tensor, lens: torch.Tensor, n
     if (q is None) != (q_out is None) or (cos is None) != (sin is None):
         raise MoEError("q and q_out, cos and sin come in pairs")
     tab = (1, 0) if cos is None else tuple(cos.shape)
+    if cos is not None and (len(tab) != 2 or 0 in tab):   # an empty one has no address, as none
+        raise MoEError("cos and sin must be [positions][half], and not empty")
     qp, ld_q, Hq, op, ld_o = None, 0, 0, None, 0
     if q is not None:
         Hq = q.shape[1]
@@ -360,7 +362,9 @@ def moe_tree_attention(desc: CacheDesc, table: torch.Tensor, lens: torch.Tensor,
     if D != desc.head_dim:
         raise MoEError("q has heads of %d, the cache of %d" % (D, desc.head_dim))
     dt = _DTYPE16[desc.type]
-    words = 0 if mask is None else mask.shape[-1]
+    words = 0 if mask is None else mask.shape[-1] if mask.dim() else 0
+    if mask is not None and words < 1:                    # an empty one has no address, as none
+        raise MoEError("mask must be [tokens][words], a word at least")
     qp, ld_q = _heads(q, N, Hq, D, dt, "q")
     op, ld_o = _heads(out, N, Hq, D, dt, "out")
     wp, wb = None, 0
