@@ -729,7 +729,8 @@ int moe_cache_append_norm(const moe_cache_t* C, const int32_t* table, int32_t ma
  * k[((p*n_heads + g)*page_size + o)*head_dim + c], value codes, transposed inside the
  * page, at v[((p*n_heads + g)*head_dim + c)*page_size + o], and the scales at
  * k_scale, v_scale[(p*n_heads + g)*page_size + o].  Slots that no token has been written
- * to may hold anything.
+ * to may hold anything.  Rows that a caller wrote have scales of 0 or between 2^-64 and 2^64, or NaN
+ * (in the attention, a value's scale below 2^-64 counts as 2^-64).
  */
 typedef struct moe_qcache {
   void*   k;            /* device int8, 16-byte aligned */

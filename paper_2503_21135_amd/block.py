@@ -197,7 +197,8 @@ class QuantPagedCache(PagedCache):
     half the memory and half of what attention reads.
 
     k      int8 [pages][heads][page_size][head_dim], v int8 [pages][heads][head_dim][page_size]
-    k_scale, v_scale  float32 [pages][heads][page_size]: a row stands for scale * codes
+    k_scale, v_scale  float32 [pages][heads][page_size]: a row stands for scale * codes.  Scales of
+           0 or between 2^-64 and 2^64 (a value's below that counts as 2^-64 in attend), or NaN
     dtype  of queries, keys, values and outputs, bfloat16 or float16
     """
 

@@ -78,6 +78,11 @@ __device__ __forceinline__ uint32_t seen16(const QArgs& a, int64_t t, int i, int
   return (bits << below | ((1u << below) - 1)) & 0xFFFFu;
 }
 
+// log2 and reciprocal of a value's scale, of 2^-64 at least: a row of zeros that came with a scale of 0
+// has its share of the sum, too.  (The logarithm of NaN, and of a negative scale, stays NaN.)
+__device__ __forceinline__ float log_of(float s) { return __builtin_elementwise_maximum(__builtin_amdgcn_logf(s), -64.f); }
+__device__ __forceinline__ float inverse_of(float s) { return fminf(__builtin_amdgcn_rcpf(s), 0x1p64f); }
+
 // lane E's value of each 16 lanes, on all of them
 template <int E>
 __device__ __forceinline__ float from_lane(float v) { return dpp<0x150 + E>(v); }
@@ -291,7 +296,7 @@ __global__ void __launch_bounds__(64 * RW * KW, RW * KW == 8 || (RW == 1 && D <=
         }
       }
       u32x4 pf[RT][2], rest[RT][2];
-      const float k2 = ks * a.scale2, lg = __builtin_amdgcn_logf(vs), rv = __builtin_amdgcn_rcpf(vs);
+      const float k2 = ks * a.scale2, lg = log_of(vs), rv = inverse_of(vs);
 #pragma unroll
       for (int rt = 0; rt < RT; rt++) {
         st.template exponents<EDGE>(rt, sc[rt], [&](int kt) { return from_lanes(k2, kt); }, [&](int kt) { return from_lanes(lg, kt); }, see[rt]);
@@ -394,8 +399,8 @@ __global__ void __launch_bounds__(64 * RW * KW, RW * KW == 8 || (RW == 1 && D <=
         }
         if (tid < kTile) {
           tile.k2[tid / 4][tid % 4] = ks * a.scale2;
-          tile.lg[tid / 4][tid % 4] = __builtin_amdgcn_logf(vs);
-          tile.rv[tid / 4][tid % 4] = __builtin_amdgcn_rcpf(vs);
+          tile.lg[tid / 4][tid % 4] = log_of(vs);
+          tile.rv[tid / 4][tid % 4] = inverse_of(vs);
         }
       }
       __syncthreads();
