@@ -835,8 +835,9 @@ int moe_qcache_keep(const moe_qcache_t* C, const int32_t* table, int32_t max_pag
  * -1, and MOE_ERR_RANGE is set in status.  A token or parent out of range is not accepted, and a sequence
  * whose rows are out of range gets n_keep 0 and next -1 (MOE_ERR_SLOT).  A sequence without new
  * tokens gets n_keep 0 and next -1.  max_new at most 1024.
- * The last row's probabilities and sums are taken in 64 bits, those of the tests from
- * fp32 exponentials summed in 64.  Results are bitwise reproducible.
+ * Exponentials and sums of the draw are taken in 64 bits.  The tests' p_i, and what is left of a row
+ * after a refusal with `draft`, have a row's sum of fp32 exponentials, added in 64 bits, for a
+ * divisor: a term e^y of it (y <= 0) is off by 2^-22 (2 + |y|) of itself at most.  Results are bitwise reproducible.
  */
 int moe_draft_verify_plan(int32_t n_seqs, int32_t n_tokens, int32_t max_new, int32_t vocab, size_t* ws_bytes);
 int moe_draft_verify(const void* logits, int32_t logits_type, int64_t ld_logits, int32_t n_tokens,

@@ -108,8 +108,10 @@ __device__ __forceinline__ float wave_max(float v) {
 // log2(e) / heat, finite for the smallest
 __device__ __forceinline__ float rate_of(float heat) { return fminf(1.44269504088896340736f / heat, 1e30f); }
 
-// The exponentials' arguments are products of an exact difference, and each is off by 2^-24 of
-// itself at most: a row's sum by about 10^-7 of itself, which the tests compare to.
+// A term e^y of a row's sum is an fp32 exponential: its argument has three roundings of 2^-24 |y| (difference,
+// rate, product) and the exponential one of 2^-23, as have the factors that bring waves and
+// blocks to one maximum, whose exponents add up to |y|: 2^-22 (2 + |y|) of itself at most.  The terms are added in
+// 64 bits (a thread's 16 or 32 in 32 bits moved sums by up to 5e-7; 64 chains of 7 27.1 us that way, 27.7 this way).
 // Reads every logit once, all loads of a thread before the first is used: 16 trees of 31 over 131072
 // fp32 (190 MB) 33.9 us, 5.6 TB/s; 64 chains of 7 over 32000 bf16 (27 MB) 10.1 us; one chain of 4
 // 4.0, a launch and two rounds of loads.
@@ -155,12 +157,11 @@ __global__ void __launch_bounds__(kThreads) stats_kernel(Args a) {
     if (__any(nan)) sum = __builtin_nan("");
   } else {
     const float rate = rate_of(heat), base = top == -INFINITY ? 0.f : top;
-    float part = 0.f;
 #pragma unroll
     for (int p = 0; p < kPieces; p++)
 #pragma unroll
-      for (int e = 0; e < M; e++) part += __builtin_amdgcn_exp2f((x[p][e] - base) * rate);
-    sum = wave_sum64(part);
+      for (int e = 0; e < M; e++) sum += static_cast<double>(__builtin_amdgcn_exp2f((x[p][e] - base) * rate));
+    sum = wave_sum64(sum);
   }
   if (tid % kWave == 0) {
     tops[tid / kWave] = top;
