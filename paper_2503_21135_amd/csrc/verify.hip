@@ -515,7 +515,8 @@ __device__ __forceinline__ int first_past(double mine, double up, double aim, in
 }
 
 // Sums that one workgroup of a launch writes and another reads.  An exchange has been performed where
-// the whole device sees it once its old value is back, which the wait is for.
+// the whole device sees it once its old value is back, which the wait is for.  (The language orders two relaxed
+// operations on different places by a release alone; that the wait is in the code is tested.)
 __device__ __forceinline__ void put_total(double* p, double v) {
   auto* at = reinterpret_cast<unsigned long long*>(p);
   const unsigned long long old = __hip_atomic_exchange(at, __builtin_bit_cast(unsigned long long, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
