@@ -782,7 +782,8 @@ int moe_qcache_read(const moe_qcache_t* C, const int32_t* table, int32_t max_pag
  * fp16 outputs up to 32 rows per key/value head (max_new * n_q_heads / n_heads; 16 at
  * head_dim 256), as a rounded weight and the rounded rest.  (Below 2^-32 of the row's largest
  * such product of weight and scale it may count as zero there.)  The weights' sum is of
- * fp32 weights, none of them left out.  Results are bitwise reproducible.
+ * fp32 weights, those of zeros too (below 2^-126 of that largest product a weight may be left out, as
+ * can be where value scales are 2^100 apart).  Results are bitwise reproducible.
  */
 int moe_qcache_attention_plan(const moe_qcache_t* C, int32_t n_q_heads, int32_t n_seqs,
                               int32_t max_new, int32_t max_len, int32_t* n_split, size_t* ws_bytes);

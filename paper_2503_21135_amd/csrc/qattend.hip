@@ -184,7 +184,7 @@ __device__ __forceinline__ f32x4 from_lanes(float v, int kt) {
 // Few rows are bound by HBM: 64 single tokens by 32 query and 8 key heads of 128 over up to 4096, 415 MB,
 // 83 us, 5.0 TB/s and up to 6.1 for longer contexts.  The next tile's
 // keys load behind this one's products (else 94 us); a third wave a SIMD would spill (105).
-// Many rows are bound by phases that hardly overlap: 4 trees of 64 over up to 32768 147 us (0.56 PFLOP/s;
+// Many rows are bound by phases that hardly overlap: 4 trees of 64 over up to 32768 147 to 151 us (0.56 PFLOP/s;
 // matrix instructions a third of a busy CU's cycles, vector ones half, LDS a third).  Tried for
 // them: one row tile's products among the other's softmax 178 us, two workgroups a CU 179, the two waves of
 // a SIMD half a tile apart 177, scales by lanes instead of LDS 170, s_setprio 172 (all against 161 then).
@@ -204,8 +204,10 @@ __global__ void __launch_bounds__(64 * RW * KW, RW * KW == 8 || (RW == 1 && D <=
     Sums sums;
   };
   constexpr bool kShared = RW > 1, kAhead = RT * D <= 128;
-  // Weights are rounded to fp16.  Few rows with fp16 outputs, which wait for HBM, add the product
-  // with what the rounding left over.
+  // Weights are rounded to fp16, as outputs are or, in bf16, to less.  Few rows with fp16 outputs, which
+  // wait for HBM, add the product with what the rounding left over; for many rows that would be half as much again
+  // of the matrix work and of the weights' (4 trees of 64 over up to 32768: a call of 212 us instead of 157,
+  // its error against 64 bits 2.1e-4, that of the output's rounding, instead of 2.9e-4).
   constexpr bool kRest = !kShared && TYPE == MOE_TYPE_FP16;
   __shared__ __attribute__((aligned(16))) char lds_bytes[kShared ? (KW > 1 ? sizeof(Lds) : sizeof(Tile) * 2) : sizeof(Sums)];
   __shared__ float stats[W][RT][16][2];

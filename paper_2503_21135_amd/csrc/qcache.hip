@@ -116,10 +116,12 @@ __device__ __forceinline__ void load_floats(const float* p, float* f) {
 // trees 15.9 us instead of 14, one token 4.7 instead of 3.4).  What the row's place alone tells is on
 // its way before positions and pages are known, and the next head's row during this one's arithmetic.
 // Prompts are bound by HBM: 8192 tokens of 32 query and 8 key heads of 128, 206 MB read and written,
-// take 48.3 us in 16 bits (4.3 TB/s), 52.2 for 185 MB in 8, where a workgroup loads nothing while it quantizes.  Trees of drafts wait for a chain of dependent loads (lengths,
-// pages and positions, rows) and store their values a slot at a time: 32 trees of 16 to 32 tokens 14 us.
-// Values in workgroups of their own took the trees 15.8 us, four heads in registers at once the
-// prompt 50 instead of 40 in 8 bits (fewer waves), six waves a SIMD spill.
+// take 48.3 us in 16 bits (4.3 TB/s), 52.1 for 185 MB in 8, where a workgroup loads nothing while it quantizes.
+// Trees of drafts (32 of 16 to 32 tokens: 14.2 to 14.7 us in 8 bits, 12.5 in 16) wait for a chain of dependent loads (lengths,
+// pages and positions, rows), store their values a slot at a time, and leave half of the card idle: a tree
+// has two tiles, the second mostly without a token, and tiles run fastest in the grid, so that workgroups with work
+// all fall on every second XCD (with sequences fastest the call and its read took 17.8 us instead of 18.9).
+// Values in workgroups of their own took the trees 15.8 us; six waves a SIMD spill.
 template <int TYPE, int D, bool Q8>
 __global__ void __launch_bounds__(4 * D) store_kernel(StoreArgs a) {
   typedef elem_t<TYPE> E;
@@ -130,8 +132,8 @@ __global__ void __launch_bounds__(4 * D) store_kernel(StoreArgs a) {
   __shared__ int64_t pages[kSlots / 32];            // first slot of each 32 in the head of its page, or -1
   __shared__ int where[kSlots];                     // position of each slot's token, or -1: no token, or one to skip
   __shared__ Two turned[D][kSlots / 2 + 2];
-  // w_k and w_q: in registers instead the prompt takes 51.9 us, not 50.7, and 8 of 300 to 600 tokens by 16 and 4
-  // heads of 256 52.3, not 49.6
+  // w_k and w_q: in registers instead a call of 8192 tokens by 32 and 8 heads of 128 takes 50.3 us, not 49.1, and
+  // one of 8 x 300 to 600 tokens by 16 and 4 heads of 256 52.3, not 49.6
   __shared__ __attribute__((aligned(16))) float norms[2][D];
   const int s = blockIdx.y, g = blockIdx.z, tid = threadIdx.x;
   bool ok;

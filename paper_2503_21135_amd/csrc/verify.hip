@@ -113,8 +113,8 @@ __device__ __forceinline__ float rate_of(float heat) { return fminf(1.4426950408
 // blocks to one maximum, whose exponents add up to |y|: 2^-22 (2 + |y|) of itself at most.  The terms are added in
 // 64 bits (a thread's 16 or 32 in 32 bits moved sums by up to 5e-7; 64 chains of 7 27.1 us that way, 27.7 this way).
 // Reads every logit once, all loads of a thread before the first is used: 16 trees of 31 over 131072
-// fp32 (190 MB) 33.9 us, 5.6 TB/s; 64 chains of 7 over 32000 bf16 (27 MB) 10.1 us; one chain of 4
-// 4.0, a launch and two rounds of loads.
+// fp32 (190 MB) 34.2 us, 5.5 TB/s; 64 chains of 7 over 32000 bf16 (27 MB) 10.8 us; one chain of 4
+// 4.1, a launch and two rounds of loads.
 template <int TYPE, int EACH>
 __global__ void __launch_bounds__(kThreads) stats_kernel(Args a) {
   __shared__ float tops[kWaves];
@@ -443,9 +443,9 @@ struct Taken {   // tokens that were refused, in LDS
   int* token;
 };
 
-// 2^y for y <= 0, by its Taylor series in ln2 (y - rint(y)) up to the 11th power: off by 7e-15 of
+// 2^y for y <= 0, by its Taylor series in ln2 (y - rint(y)) up to the 11th power: off by 9e-15 of
 // itself at most, and a rounding of 2^-53 or two.  The library's exp takes about twice the
-// instructions, and a pass one a token: 64 chains of 7 28.7 us with it, 27.8 with this; 16 trees of 31 82.7 and 80.9.
+// instructions, and a pass one a token: calls of 64 chains of 7 take 30.0 us with it, 27.7 with this; 16 trees of 31 85.0 and 80.7.
 __device__ __forceinline__ double power(double y) {
   constexpr double kTerms[12] = {1.0, 0.6931471805599453, 0.24022650695910072, 0.05550410866482158, 0.009618129107628477, 0.0013333558146428443, 0.0001540353039338161, 1.5252733804059841e-05, 1.321548679014431e-06, 1.01780860092397e-07, 7.054911620801123e-09, 4.4455382718708116e-10};   // (ln 2)^k / k!
   y = fmax(y, -1100.);   // 0, of -infinity too
@@ -867,15 +867,16 @@ extern "C" int moe_draft_verify(const void* logits, int32_t logits_type, int64_t
     else launch_stats<MOE_TYPE_FP16>(wide, most, s, a);
   }
   // The first pass begins the walk where that takes each of its workgroups no more than a few loads (one
-  // chain of 4 over 32000 tokens 17.4 us, with a launch for it 19.5; 64 chains of 7 29.4 and 31.4); else a launch with a lane for every
+  // chain of 4 over 32000 tokens 16.0 us, with a launch for it 18.2; 64 chains of 7 27.7 and 30.7); else a launch with a lane for every
   // block of a sequence's rows, if that takes no more than a workgroup.
   const int64_t parts = static_cast<int64_t>(most) * a.blocks;
   const bool with_pass = most > 0 && u && parts <= 512;
   if (!with_pass) hipLaunchKernelGGL(walk_kernel, dim3(n_seqs), dim3(parts > kThreads ? 1024 : kThreads), most * kDraftBytes, s, a, most);
   if (most > 0 && u) {
     // A drawn tree takes a pass for each refusal of its walk.  What the launches leave is summed by one
-    // workgroup (0.7 us a chunk); one with nothing to do takes 2 us.  16 trees of 31 over 131072 tokens:
-    // 80 us with 4, 85 with 6, or, where a walk refuses 5 times, 127 with 4, 93 with 6.
+    // workgroup (0.7 us a chunk: 88 us a refusal over 131072 tokens, so that a walk that refuses all of 64 drafts
+    // below one row there takes 5.1 ms); one with nothing to do takes 2 us.  16 trees of 31 over 131072 tokens:
+    // 77.6 us with 4, 80.7 with 6, or, where every walk refuses 5 times, 180 with 4, 97 with 6.
     const int passes = draft && parents ? std::min(most, a.chunks == 1 ? 1 : a.chunks <= 4 ? 3 : a.chunks <= 32 ? 4 : 6) : 1;
     const int bytes = most * kDraftBytes;
     const int each = pass_each_of(n_seqs, vocab);
